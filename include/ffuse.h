@@ -220,6 +220,56 @@ int ffuse_conv_chain(const void* X, const void* W1, const void* W2, int act, int
 int ffuse_conv_chain_f16(const void* X, const void* W1, const void* W2, int act, int64_t B, int64_t H,
                          int64_t W, int64_t IC, int64_t OC1, int64_t OC2, int k1, int k2, void* Y, void* stream);
 
+/* ---- matrix products grouped by expert: R rows sorted by expert, E weight matrices.  offsets[0 .. E] (int32, DEVICE
+ *      memory, read when the kernel runs) are the boundaries: rows offsets[e] .. offsets[e + 1] - 1 are multiplied by
+ *      matrix e.  They must not decrease and must lie in 0 .. R; others are clamped to that (which rows then belong to
+ *      which expert is unspecified, every access stays inside the tensors).  Groups may be empty; rows before offsets[0]
+ *      and from offsets[E] on belong to no group, and what the output holds there is left as it is.
+ *      dtype: FFUSE_DT_BF16 or FFUSE_DT_F16; fp32 sums, rounded once.  R >= 0 (R = 0: nothing to do, A and C may be
+ *      NULL), 1 <= E <= 1024, K and N multiples of 8 from 8 to 2^20, ONE matrix below 2 GiB (all of them together, and
+ *      the rows, may be larger).  Errors, alignment and stream as above.  No workspace but ffuse_grouped_ffn's.
+ *
+ *   ffuse_grouped_gemm      Y[r] = act(X[r] W[e]) (.* X[r] W3[e])      X[R][K], W[E][K][N], W3 like W or NULL, Y[R][N]
+ *   ffuse_grouped_gemm_dx   dX[r] = dY[r] W[e]^T                        the plain product's gradients: of its input, dX[R][K],
+ *   ffuse_grouped_gemm_dw   dW[e] = X_e^T dY_e                          and of its weights, dW[E][K][N] (zeros for an empty
+ *                                                                       group; all of dW is overwritten, also when R = 0)
+ *   ffuse_grouped_ffn       Y[r] = (act(X[r] W1[e]) (.* X[r] W3[e])) W2[e]   the chain as two products; the intermediate
+ *                           H[R][N1], rounded to the operand type, lives in `workspace` (ffuse_grouped_workspace_bytes,
+ *                           16-byte aligned; calls that overlap in time need different ones; it may be one that other
+ *                           calls use in between).  W1, W3 [E][K][N1], W2 [E][N1][N2]. ------------------------------- */
+int ffuse_grouped_gemm(int dtype, const void* X, const void* W, const void* W3 /* NULL = not gated */, const int32_t* offsets, int act,
+                       int64_t R, int64_t E, int64_t K, int64_t N, void* Y, void* stream);
+int ffuse_grouped_gemm_dx(int dtype, const void* dY, const void* W, const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N,
+                          void* dX, void* stream);
+int ffuse_grouped_gemm_dw(int dtype, const void* X, const void* dY, const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N,
+                          void* dW, void* stream);
+size_t ffuse_grouped_workspace_bytes(int dtype, int64_t R, int64_t N1);   /* 0: not a problem of ffuse_grouped_ffn */
+int ffuse_grouped_ffn(int dtype, const void* X, const void* W1, const void* W3 /* NULL = not gated */, const void* W2,
+                      const int32_t* offsets, int act, int64_t R, int64_t E, int64_t K, int64_t N1, int64_t N2, void* Y,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- products in 8-bit floating point (e4m3: 4 exponent bits, 3 mantissa bits, largest number 448, no infinities) with
+ *      a scale for each block of 128 along the contraction.
+ *
+ *   ffuse_fp8_quantize   X[M][K] (dtype: FFUSE_DT_BF16 or FFUSE_DT_F16) -> Q and scale, with x ~ q * scale.  Blocks are
+ *      block_rows x 128: 1 (an operand's rows) or 128 (weights).  transpose = 0: Q[M][Kp], Kp = K rounded up to 16 (zeros
+ *      in between), scale[ceil(K/128)][ceil(M/block_rows)].  transpose = 1: the same of X^T: Q[K][Mp], scale[ceil(M/128)]
+ *      [ceil(K/block_rows)].  The scale is the smallest power of two, 2^-126 at least, that brings the largest finite
+ *      magnitude of the block to 448 or below (1 for a block of zeros): dividing by it is exact, the quotient is rounded once, to nearest
+ *      even.  Infinities and NaN do not count for the scale and become NaN.  M >= 0, K a multiple of 8 up to 2^20.
+ *   ffuse_gemm_fp8       Y[m][n] = sum over blocks b of sa[b][m] sb[b][n / b_block] (sum over k in b of A[m][k] B[n][k])
+ *      A[M][K], B[N][K] in e4m3, scales in fp32 (any, not only powers of two) laid out as above, b_block 1 or 128, Y[M][N] of
+ *      type dtype (bf16 or fp16), rounded once.  M >= 0, K a multiple of 16, N of 8.  An inference product has A = rows of
+ *      X by 1 x 128 and B = W^T by 128 x 128; its gradients dX = dY W^T (B = W untransposed) and dW = X^T dY (both
+ *      operands transposed, by 1 x 128) are this product too.
+ *   ffuse_grouped_gemm_fp8   the same with the rows of A grouped by expert as above: B[E][N][K], sb[E][ceil(K/128)][...]. -- */
+int ffuse_fp8_quantize(int dtype, const void* X, int64_t M, int64_t K, int block_rows, int transpose, void* Q, float* scale,
+                       void* stream);
+int ffuse_gemm_fp8(int dtype, const void* A, const float* sa, const void* B, const float* sb, int b_block, int64_t M, int64_t K,
+                   int64_t N, void* Y, void* stream);
+int ffuse_grouped_gemm_fp8(int dtype, const void* A, const float* sa, const void* B, const float* sb, int b_block,
+                           const int32_t* offsets, int64_t R, int64_t E, int64_t K, int64_t N, void* Y, void* stream);
+
 /* ---- workspace.  ffuse_workspace_bytes: bytes the given problem needs (fused path when
  *      unfused == 0; with unfused != 0 the two-launch path's intermediate, partial-sum planes
  *      and flags).  ffuse_set_workspace: registers a caller-owned device buffer with the

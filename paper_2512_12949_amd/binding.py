@@ -28,6 +28,8 @@ EXPORTS = [
     "ffuse_status_string", "ffuse_version",
     "ffuse_ffn_ws", "ffuse_ffn_unfused_ws", "ffuse_debug_barrier", "ffuse_set_objective",
     "ffuse_loop_schedule_count", "ffuse_cluster_exchange", "ffuse_ffn_static", "ffuse_calibrate",
+    "ffuse_grouped_gemm", "ffuse_grouped_gemm_dx", "ffuse_grouped_gemm_dw", "ffuse_grouped_ffn", "ffuse_grouped_workspace_bytes",
+    "ffuse_fp8_quantize", "ffuse_gemm_fp8", "ffuse_grouped_gemm_fp8",
 ]
 
 
@@ -131,6 +133,19 @@ def lib():
         L.ffuse_calibrate.argtypes = [ci, ci, vp, i64, i64, vp, ctypes.POINTER(ctypes.c_double), vp]
         L.ffuse_debug_barrier.restype = ci
         L.ffuse_debug_barrier.argtypes = [ci, ctypes.c_uint]
+        for name, args in (
+                ("ffuse_grouped_gemm", [ci, vp, vp, vp, vp, ci, i64, i64, i64, i64, vp, vp]),
+                ("ffuse_grouped_gemm_dx", [ci, vp, vp, vp, i64, i64, i64, i64, vp, vp]),
+                ("ffuse_grouped_gemm_dw", [ci, vp, vp, vp, i64, i64, i64, i64, vp, vp]),
+                ("ffuse_grouped_ffn", [ci, vp, vp, vp, vp, vp, ci, i64, i64, i64, i64, i64, vp, vp, ctypes.c_size_t, vp]),
+                ("ffuse_fp8_quantize", [ci, vp, i64, i64, ci, ci, vp, vp, vp]),
+                ("ffuse_gemm_fp8", [ci, vp, vp, vp, vp, ci, i64, i64, i64, vp, vp]),
+                ("ffuse_grouped_gemm_fp8", [ci, vp, vp, vp, vp, ci, vp, i64, i64, i64, i64, vp, vp])):
+            f = getattr(L, name)
+            f.restype = ci
+            f.argtypes = args
+        L.ffuse_grouped_workspace_bytes.restype = ctypes.c_size_t
+        L.ffuse_grouped_workspace_bytes.argtypes = [ci, i64, i64]
         _lib = L
     return _lib
 
@@ -417,6 +432,166 @@ def ffuse_conv_chain(X, W1, W2, act, Y, stream=None, check=True):
 
 def ffuse_conv_chain_f16(X, W1, W2, act, Y, stream=None, check=True):
     return _conv("ffuse_conv_chain_f16", X, W1, W2, act, Y, stream, check)
+
+
+# ---- products grouped by expert, and 8-bit products.  Sizes come from the tensors, which are checked here: what the C ABI
+# sees of a tensor is an address.
+
+def _want(name, t, shape, dtype):
+    """Raises unless t is a contiguous tensor of this shape and type on the current device."""
+    import torch
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} is needed, not {t.dtype} {tuple(t.shape)}"
+                         f"{'' if t.is_contiguous() else ', not contiguous'}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, not on the current device")
+
+
+def _operand_dtype(dtype):
+    import torch
+    t = {DT_BF16: torch.bfloat16, DT_F16: torch.float16}.get(int(dtype))
+    if t is None:
+        raise ValueError(f"dtype {dtype}: DT_BF16 or DT_F16")
+    return t
+
+
+def _want_dims(name, t, n):
+    if t.dim() != n:
+        raise ValueError(f"{name}: {n} dimensions are needed, not {t.dim()}")
+
+
+def _rc(name, rc, check):
+    if check and rc != 0:
+        _check(rc, name)
+    return rc
+
+
+def ffuse_grouped_gemm(dtype, X, W, W3, offsets, act, Y, stream=None, check=True):
+    """Y[r] = act(X[r] W[e]) (.* X[r] W3[e]) for the rows r = offsets[e] .. offsets[e + 1] - 1 of each expert e.
+
+    X [R][K], W and W3 (or None) [E][K][N], offsets [E + 1] int32, all on the device; Y [R][N] (rows of no group are left as they are)."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("X", X, 2)
+    _want_dims("W", W, 3)
+    (R, K), (E, _, N) = X.shape, W.shape
+    for name, x, shape, kind in (("X", X, (R, K), t), ("W", W, (E, K, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("Y", Y, (R, N), t)):
+        _want(name, x, shape, kind)
+    if W3 is not None:
+        _want("W3", W3, (E, K, N), t)
+    return _rc("ffuse_grouped_gemm", lib().ffuse_grouped_gemm(int(dtype), _addr(X), _addr(W), _addr(W3), _addr(offsets), int(act), R, E, K, N, _addr(Y),
+                                                              _stream_addr(stream)), check)
+
+
+def ffuse_grouped_gemm_dx(dtype, dY, W, offsets, dX, stream=None, check=True):
+    """dX[r] = dY[r] W[e]^T: the gradient of the plain product's input.  dY [R][N], W [E][K][N], dX [R][K]."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("dY", dY, 2)
+    _want_dims("W", W, 3)
+    (R, N), (E, K, _) = dY.shape, W.shape
+    for name, x, shape, kind in (("dY", dY, (R, N), t), ("W", W, (E, K, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("dX", dX, (R, K), t)):
+        _want(name, x, shape, kind)
+    return _rc("ffuse_grouped_gemm_dx", lib().ffuse_grouped_gemm_dx(int(dtype), _addr(dY), _addr(W), _addr(offsets), R, E, K, N, _addr(dX),
+                                                                    _stream_addr(stream)), check)
+
+
+def ffuse_grouped_gemm_dw(dtype, X, dY, offsets, dW, stream=None, check=True):
+    """dW[e] = X_e^T dY_e: the gradient of the plain product's weights, zeros for an expert without rows.  X [R][K], dY [R][N], dW [E][K][N]."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("X", X, 2)
+    _want_dims("dW", dW, 3)
+    (R, K), (E, _, N) = X.shape, dW.shape
+    for name, x, shape, kind in (("X", X, (R, K), t), ("dY", dY, (R, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("dW", dW, (E, K, N), t)):
+        _want(name, x, shape, kind)
+    return _rc("ffuse_grouped_gemm_dw", lib().ffuse_grouped_gemm_dw(int(dtype), _addr(X), _addr(dY), _addr(offsets), R, E, K, N, _addr(dW),
+                                                                    _stream_addr(stream)), check)
+
+
+def ffuse_grouped_workspace_bytes(dtype, R, N1) -> int:
+    return int(lib().ffuse_grouped_workspace_bytes(int(dtype), R, N1))
+
+
+def ffuse_grouped_ffn(dtype, X, W1, W3, W2, offsets, act, Y, workspace, stream=None, check=True):
+    """Y[r] = (act(X[r] W1[e]) (.* X[r] W3[e])) W2[e], the chain by expert.  W1, W3 (or None) [E][K][N1], W2 [E][N1][N2];
+    workspace: a device tensor of ffuse_grouped_workspace_bytes(dtype, R, N1) bytes."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("X", X, 2)
+    _want_dims("W2", W2, 3)
+    (R, K), (E, N1, N2) = X.shape, W2.shape
+    for name, x, shape, kind in (("X", X, (R, K), t), ("W1", W1, (E, K, N1), t), ("W2", W2, (E, N1, N2), t), ("offsets", offsets, (E + 1,), torch.int32),
+                                 ("Y", Y, (R, N2), t)):
+        _want(name, x, shape, kind)
+    if W3 is not None:
+        _want("W3", W3, (E, K, N1), t)
+    nbytes = 0
+    if workspace is not None:
+        _want("workspace", workspace, workspace.shape, workspace.dtype)
+        nbytes = workspace.numel() * workspace.element_size()
+    return _rc("ffuse_grouped_ffn", lib().ffuse_grouped_ffn(int(dtype), _addr(X), _addr(W1), _addr(W3), _addr(W2), _addr(offsets), int(act), R, E, K, N1, N2,
+                                                            _addr(Y), _addr(workspace), nbytes, _stream_addr(stream)), check)
+
+
+def ffuse_fp8_quantize(dtype, X, Q, scale, block_rows=1, transpose=False, stream=None, check=True):
+    """X [M][K] as e4m3 numbers Q [M][K rounded up to 16] and fp32 scales [ceil(K / 128)][ceil(M / block_rows)], one for
+    each block of block_rows (1 or 128) x 128; with transpose the same of X^T."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("X", X, 2)
+    M, K = X.shape
+    m, k = (K, M) if transpose else (M, K)
+    rows = 128 if block_rows == 128 else 1
+    for name, x, shape, kind in (("X", X, (M, K), t), ("Q", Q, (m, (k + 15) // 16 * 16), torch.float8_e4m3fn),
+                                 ("scale", scale, ((k + 127) // 128, (m + rows - 1) // rows), torch.float32)):
+        _want(name, x, shape, kind)
+    return _rc("ffuse_fp8_quantize", lib().ffuse_fp8_quantize(int(dtype), _addr(X), M, K, int(block_rows), int(bool(transpose)), _addr(Q), _addr(scale),
+                                                              _stream_addr(stream)), check)
+
+
+def _fp8_block(sb, kb, N):
+    """1 or 128: the rows of B that share a scale, from the shape of the scales."""
+    for block in (128, 1):
+        if tuple(sb.shape[-2:]) == (kb, (N + block - 1) // block):
+            return block
+    raise ValueError(f"scales of B: the last dimensions are needed as {(kb, (N + 127) // 128)} or {(kb, N)}, not {tuple(sb.shape[-2:])}")
+
+
+def ffuse_gemm_fp8(dtype, A, sa, B, sb, Y, stream=None, check=True):
+    """Y [M][N] (DT_BF16 or DT_F16) = the product of A [M][K] and B [N][K], both e4m3, sa [ceil(K / 128)][M] and sb
+    [ceil(K / 128)][ceil(N / 128) or N] their scales."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("A", A, 2)
+    _want_dims("B", B, 2)
+    (M, K), (N, _) = A.shape, B.shape
+    kb = (K + 127) // 128
+    block = _fp8_block(sb, kb, N)
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    for name, x, shape, kind in (("A", A, (M, K), e4m3), ("sa", sa, (kb, M), f32), ("B", B, (N, K), e4m3), ("sb", sb, (kb, (N + block - 1) // block), f32),
+                                 ("Y", Y, (M, N), t)):
+        _want(name, x, shape, kind)
+    return _rc("ffuse_gemm_fp8", lib().ffuse_gemm_fp8(int(dtype), _addr(A), _addr(sa), _addr(B), _addr(sb), block, M, K, N, _addr(Y), _stream_addr(stream)),
+               check)
+
+
+def ffuse_grouped_gemm_fp8(dtype, A, sa, B, sb, offsets, Y, stream=None, check=True):
+    """ffuse_gemm_fp8 with the rows of A grouped by expert: B [E][N][K], sb [E][ceil(K / 128)][ceil(N / 128) or N]."""
+    import torch
+    t = _operand_dtype(dtype)
+    _want_dims("A", A, 2)
+    _want_dims("B", B, 3)
+    _want_dims("sb", sb, 3)
+    (R, K), (E, N, _) = A.shape, B.shape
+    kb = (K + 127) // 128
+    block = _fp8_block(sb, kb, N)
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    for name, x, shape, kind in (("A", A, (R, K), e4m3), ("sa", sa, (kb, R), f32), ("B", B, (E, N, K), e4m3),
+                                 ("sb", sb, (E, kb, (N + block - 1) // block), f32), ("offsets", offsets, (E + 1,), torch.int32), ("Y", Y, (R, N), t)):
+        _want(name, x, shape, kind)
+    return _rc("ffuse_grouped_gemm_fp8", lib().ffuse_grouped_gemm_fp8(int(dtype), _addr(A), _addr(sa), _addr(B), _addr(sb), block, _addr(offsets), R, E, K, N,
+                                                                      _addr(Y), _stream_addr(stream)), check)
 
 
 def ffuse_profile_enable(on: bool):

@@ -473,6 +473,33 @@ int check_ws_arg(const void* ws, size_t bytes) {
 
 }  // namespace
 
+namespace ffuse {
+
+int device_ready(int* cus) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    const int rc = check_arch();
+    *cus = g.cus;
+    return rc;
+}
+
+void workspace_overwritten(void* p, size_t bytes, hipStream_t st) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    const bool recorded = stream_is_capturing(st);
+    if (recorded) workspace_record(p, bytes);   // (so that a later call on it knows)
+    const char* a = static_cast<const char*>(p);
+    const auto dirty = [&](Workspace& w) {
+        const char* b = static_cast<const char*>(w.ptr);
+        if (!w.ptr || a >= b + w.bytes || b >= a + bytes) return;
+        w.zero = 0;
+        w.small_flags = nullptr;
+        if (recorded) w.in_graph = true;
+    };
+    dirty(g.reg);
+    for (Workspace& w : g.seen) dirty(w);
+}
+
+}  // namespace ffuse
+
 extern "C" {
 
 int ffuse_ffn(const void* X, const void* W1, const void* W3, const void* W2, int act, int64_t M, int64_t K, int64_t N1,

@@ -1,0 +1,114 @@
+// Rows grouped by expert: what the kernels that multiply each group of rows by a matrix of its own share -- the
+// group boundaries, read on the device, and the map from work items to (group, row block, column block).
+//
+// offsets[0 .. E] are the boundaries: group e is rows offsets[e] .. offsets[e + 1] - 1.  They are data, so nothing
+// the host has checked: a boundary is clamped to 0 .. R and to the largest one before it, which makes every group a
+// range inside the tensor, and the groups disjoint, whatever the values are.
+#pragma once
+#include "ffuse_dev.h"
+
+namespace ffuse {
+
+static constexpr int kMaxGroups = 1024;   // groups of a call: their boundaries are kept in LDS
+static constexpr int kGroupBand = 8;      // row blocks that share their column blocks in an XCD's L2 at a time
+
+// LDS bytes of the tables below
+__host__ __device__ inline int group_table_bytes(int E) { return 4 * (2 * E + 1); }
+
+struct Groups {
+    int* start;   // [E + 1]: the clamped boundaries
+    int* tiles;   // [E]: row blocks of the groups up to and including this one
+    int E;
+};
+
+// Fills the tables; the whole workgroup calls it, the first wave works.  offsets == nullptr: one group of all R rows.
+__device__ __forceinline__ void scan_groups(Groups& g, char* table, const int32_t* offsets, int E, int R, int bm, int tid) {
+    g.start = reinterpret_cast<int*>(table);
+    g.tiles = g.start + E + 1;
+    g.E = E;
+    if (tid < 64) {
+        int most = 0, sum = 0;   // of the groups before this round of 64
+        for (int base = 0; base < E; base += 64) {
+            const int e = base + tid;
+            const bool live = e < E;
+            int lo = 0, hi = R;
+            if (offsets) {
+                lo = live ? min(max(offsets[e], 0), R) : 0;
+                hi = live ? min(max(offsets[e + 1], 0), R) : 0;
+            }
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(lo, d);
+                if (tid >= d) lo = max(lo, up);
+            }
+            lo = max(lo, most);
+            hi = max(lo, hi);
+            int n = live ? (hi - lo + bm - 1) / bm : 0;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(n, d);
+                if (tid >= d) n += up;
+            }
+            n += sum;
+            if (live) {
+                g.start[e] = lo;
+                g.tiles[e] = n;
+                if (e == E - 1) g.start[E] = hi;
+            }
+            most = __shfl(lo, 63);
+            sum = __shfl(n, 63);
+        }
+    }
+    __syncthreads();
+}
+
+struct GroupItem {
+    int e;           // group
+    int64_t row0;    // first row of the block
+    int rows;        // rows of the group from there on (more than the block holds, or fewer)
+    int col;         // column block
+};
+
+// Item `idx` of XCD `xcd`: the items of an XCD are consecutive, the row blocks of a group in bands of kGroupBand,
+// column block by column block, so that the 32 workgroups of an XCD work on a patch of a band and a few column
+// blocks and fetch each panel of either operand into its L2 once.  ncol: column blocks.
+__device__ __forceinline__ bool group_item(const Groups& g, int bm, int ncol, int xcd, int idx, GroupItem& it) {
+    const int total = g.tiles[g.E - 1] * ncol;
+    const int per = (total + 7) >> 3;
+    const int v = xcd * per + idx;
+    if (idx >= per || v >= total) return false;
+    const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+    int e = 0;       // groups that end at or before the item
+    for (int base = 0; base < g.E; base += 64) {
+        const int i = base + lane;
+        const uint64_t before = __ballot(i < g.E && g.tiles[i < g.E ? i : 0] * ncol <= v);
+        e += __popcll(before);
+        if (before != ~0ull) break;
+    }
+    e = __builtin_amdgcn_readfirstlane(e);
+    const int t0 = __builtin_amdgcn_readfirstlane(e ? g.tiles[e - 1] : 0), nt = __builtin_amdgcn_readfirstlane(g.tiles[e]) - t0;
+    const int w = v - t0 * ncol, band = w / (kGroupBand * ncol), in = w - band * kGroupBand * ncol;
+    const int h = min(kGroupBand, nt - band * kGroupBand);
+    const int c = in / h, r = band * kGroupBand + in - c * h;
+    const int first = __builtin_amdgcn_readfirstlane(g.start[e]), last = __builtin_amdgcn_readfirstlane(g.start[e + 1]);
+    it.e = e;
+    it.row0 = (int64_t)first + (int64_t)r * bm;
+    it.rows = last - first - r * bm;
+    it.col = c;
+    return true;
+}
+
+// ---- host side of the launches
+// row blocks of bm rows that R rows in at most E groups can come to: a group has a row at least
+inline int64_t most_row_blocks(int64_t R, int64_t E, int bm) {
+    const int64_t groups = R < E ? R : E;
+    return groups + (R - groups) / bm;
+}
+// persistent workgroups: as many as fit, a multiple of eight (an XCD each), no more than there can be items
+inline int persistent_grid(int64_t items, int cus, int per_cu) {
+    const int64_t most = (int64_t)cus * per_cu;
+    const int64_t n = items < most ? items : most;
+    return (int)((n + 7) / 8 * 8);
+}
+
+}  // namespace ffuse

@@ -141,6 +141,35 @@ hipError_t launch_fused_exchange(int dtype, const ExchangeArgs& a, int wgs_per_g
 hipError_t launch_fused_reduce(int dtype, const FusedArgs& a, int bm, int bh, hipStream_t st);
 hipError_t launch_finalize(int dtype, float* sums, void* Y, int64_t count, hipStream_t st);
 
+// matrix products grouped by expert (ffuse_grouped.hip): rows of group e are offsets[e] .. offsets[e + 1] - 1
+struct GroupedArgs {
+    const void* A;            // forward, weights: X [R][K]; input: dY [R][N]
+    const void* W;            // forward, input: [E][K][N]; weights: dY [R][N]
+    const void* W3;           // forward: nullptr, or the multiplying branch's [E][K][N]
+    const int32_t* offsets;   // [E + 1], device
+    void* C;                  // forward: Y [R][N]; input: dX [R][K]; weights: dW [E][K][N]
+    int R, E, K, N;
+    int act;
+};
+hipError_t launch_grouped_forward(int dtype, const GroupedArgs& a, int cus, hipStream_t st);
+hipError_t launch_grouped_input(int dtype, const GroupedArgs& a, int cus, hipStream_t st);
+hipError_t launch_grouped_weights(int dtype, const GroupedArgs& a, hipStream_t st);
+
+// products in e4m3 with a scale per block of 128 along the contraction (ffuse_fp8.hip)
+struct Fp8Args {
+    const void* A;            // [R][K] bytes
+    const float* sa;          // [ceil(K / 128)][R]
+    const void* B;            // [E][N][K] bytes
+    const float* sb;          // [E][ceil(K / 128)][ceil(N / block)]
+    const int32_t* offsets;   // [E + 1], device; nullptr: one group of all rows
+    void* Y;                  // [R][N]
+    int R, E, K, N;
+    int block;                // rows of B that share a scale: 1 or 128
+};
+hipError_t launch_fp8_product(int dtype, const Fp8Args& a, int cus, hipStream_t st);
+// X [M][K] -> Q [M][K rounded up to 16] and scale [ceil(K / 128)][ceil(M / block)], or the same of X^T
+hipError_t launch_fp8_quantize(int dtype, const void* X, int64_t M, int64_t K, int block, bool transpose, void* Q, float* scale, hipStream_t st);
+
 // Launch of a persistent kernel whose workgroups wait for each other: every workgroup must
 // be resident at once.  The grid is checked against the occupancy the runtime reports
 // (hipErrorCooperativeLaunchTooLarge otherwise) and then launched as an ordinary kernel,
@@ -152,6 +181,12 @@ hipError_t launch_resident(const void* fn, int grid, void** params, hipStream_t 
 // zero fill with a kernel (safe to record into a captured graph, unlike a memset node);
 // bytes must be a multiple of 16
 hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);
+
+// FFUSE_OK and the number of compute units where the current device is one the kernels are for, or a status
+int device_ready(int* cus);
+// A call of another kind is about to write into [p, p + bytes) on `st`: what the library remembers about workspaces
+// there no longer holds, nor will it between calls once the writing is part of a graph.
+void workspace_overwritten(void* p, size_t bytes, hipStream_t st);
 
 // fp32 debug path
 hipError_t launch_fused_f32(const FusedArgs& a, float* Y, hipStream_t st);
