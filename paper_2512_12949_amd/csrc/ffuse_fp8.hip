@@ -31,6 +31,11 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
 // A stage is 128 k: BM + BN rows of 128 bytes, laid out as RowGemm's, and behind them their BM + BN scales of that block.
 // Computed transposed like the other block GEMMs: the MFMA "A" operand is B, so that a lane has four neighbouring
 // columns of one row of Y.
+//
+// A step multiplies one stage, 16 rows after 16 rows: the fragments of the tile's columns stay in registers, those of the next
+// 16 rows are read under the MFMAs of the present ones, and each MFMA is followed by the multiply-adds of the one four before
+// it.  The workgroup meets before the last 16 rows, whose fragments are in registers by then: the next stage has landed, the
+// present one is free for the loads of the stage NS further on, and the last MFMAs cover the reads of the next step's first fragments.
 template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct Fp8Gemm {
     static constexpr int NW = WM * WN, WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wave issues the same number of loads");
@@ -40,10 +45,15 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
     static constexpr int SA = (BM + 63) / 64, SB = (BN + 63) / 64;        // scale load instructions of a stage: 64 rows each
     static constexpr int SI = (SA + SB + NW - 1) / NW;                    // ... per wave (some are issued twice)
     static constexpr int NLOAD = XI + BI + SI;
-    static constexpr int XB = BM * 128, SOFF = XB + BN * 128, STAGE = SOFF + (SA + SB) * 256, LDS_BYTES = NS * STAGE;
-    static_assert(NS >= 2 && (NS - 1) * NLOAD <= 63, "the vmcnt field holds 6 bits");
+    static constexpr int XB = BM * 128, SOFF = XB + BN * 128, STAGE = SOFF + (SA + SB) * 256;
     static constexpr int ROW = WNR * 2, SLOTS = ROW / 8;                  // epilogue: bytes and 8-byte slots of a staged row
-    static_assert(NW * 16 * ROW <= LDS_BYTES && (ROW == 64 || ROW == 128), "the epilogue stages 16 rows a wave");
+    static constexpr int EPI = NS * STAGE, LDS_BYTES = EPI + NW * 16 * ROW;
+    static_assert(ROW == 64 || ROW == 128, "the epilogue's swizzle");
+    static constexpr int LPR = ROW / 16, RPI = 64 / LPR;                  // lanes a row and rows an instruction on the way out
+    static constexpr int STORES = MT * (16 / RPI);
+    static_assert(NS >= 2 && (NS - 1) * NLOAD + STORES <= 63, "the vmcnt field holds 6 bits");
+    static_assert(MT % 2 == 0, "the last rows' fragments and the next step's first lie in different registers");
+    static constexpr int NM = MT * HT, LAG = HT < 4 ? HT : 4;             // MFMAs a step; parts in flight
 
     struct Ctx {
         __amdgpu_buffer_rsrc_t rx, rw;
@@ -53,7 +63,7 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
         uint32_t xoff[XI], boff[BI], soff[SI];
         int ck, K;
         uint32_t lds_a, lds_b;
-        uint32_t rdx[MT], rdw[HT];
+        uint32_t rdx, rdw;             // this lane's first row of either operand in a stage (16 rows on: 2048 bytes, the same swizzle)
         uint32_t sx;                   // LDS offset of this lane's row scale in a stage
         uint32_t sw;                   // ... of its first column scale
     };
@@ -70,16 +80,8 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
         c.ck = 16 * ((lane & 7) ^ (((wave & 1) << 2) | (lane >> 4)));
         c.lds_a = (uint32_t)wave * 1024u;
         c.lds_b = XB + (uint32_t)wave * 1024u;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t r = wm * WMR + 16 * mt + x;
-            c.rdx[mt] = r * 128u + ((g ^ ((r >> 1) & 7u)) << 4);
-        }
-#pragma unroll
-        for (int ht = 0; ht < HT; ++ht) {
-            const uint32_t r = wn * WNR + 16 * ht + x;
-            c.rdw[ht] = XB + r * 128u + ((g ^ ((r >> 1) & 7u)) << 4);
-        }
+        c.rdx = (wm * WMR + x) * 128u + ((g ^ ((x >> 1) & 7u)) << 4);
+        c.rdw = XB + (wn * WNR + x) * 128u + ((g ^ ((x >> 1) & 7u)) << 4);
         c.sx = SOFF + 4u * (uint32_t)(wm * WMR + x);
         c.sw = SOFF + SA * 256u + 4u * (uint32_t)(wn * WNR + (BLOCK == 1 ? 4 * g : 0));
     }
@@ -101,89 +103,120 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
             c.soff[j] = 4u * (uint32_t)(i < SA ? min(64 * i + lane, have_a - 1) : min(64 * (i - SA) + lane, have_b - 1) / BLOCK);
         }
     }
-    // all loads of the stage of block b
-    static __device__ __forceinline__ void issue(const Ctx& c, uint32_t stage, int b, int tid) {
-        const bool ok = 128 * b + c.ck < c.K;
+    // Load i of the stage of block b.  One past the last is issued all the same, out of range: it fetches nothing and writes zeros
+    // to a place that nobody reads, and every step has the same number of loads in flight.
+    static __device__ __forceinline__ void issue_one(const Ctx& c, uint32_t stage, int b, int i, int wave) {
         const uint32_t k = 128u * (uint32_t)b;
-#pragma unroll
-        for (int i = 0; i < XI; ++i) lds_load16(c.rx, ok ? c.xoff[i] + k : kOob, stage + c.lds_a + (uint32_t)(i * NW) * 1024u);
-#pragma unroll
-        for (int i = 0; i < BI; ++i) lds_load16(c.rw, ok ? c.boff[i] + k : kOob, stage + c.lds_b + (uint32_t)(i * NW) * 1024u);
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-#pragma unroll
-        for (int j = 0; j < SI; ++j) {
-            const int i = (wave * SI + j) % (SA + SB);
-            const __amdgpu_buffer_rsrc_t r = i < SA ? make_rsrc(c.sa + b * c.sa_step, c.have_a) : make_rsrc(c.sb + b * c.sb_step, c.have_b);
-            lds_load4(r, c.soff[j], stage + SOFF + 256u * (uint32_t)i);
+        if (i < XI) lds_load16(c.rx, 128 * b + c.ck < c.K ? c.xoff[i] + k : kOob, stage + c.lds_a + (uint32_t)(i * NW) * 1024u);
+        else if (i < XI + BI) lds_load16(c.rw, 128 * b + c.ck < c.K ? c.boff[i - XI] + k : kOob, stage + c.lds_b + (uint32_t)((i - XI) * NW) * 1024u);
+        else {
+            const int j = i - XI - BI, n = (wave * SI + j) % (SA + SB);
+            const bool ok = 128 * b < c.K;
+            const __amdgpu_buffer_rsrc_t r = n < SA ? make_rsrc(c.sa + b * c.sa_step, ok ? c.have_a : 0u) : make_rsrc(c.sb + b * c.sb_step, ok ? c.have_b : 0u);
+            lds_load4(r, c.soff[j], stage + SOFF + 256u * (uint32_t)n);
         }
     }
-    static __device__ __forceinline__ i32x8 frag(const char* stage, uint32_t off) {
-        const i32x4 lo = lds_read16<i32x4>(stage, off), hi = lds_read16<i32x4>(stage, off ^ 64u);
+    // the loads of an item's first NS stages
+    static __device__ __forceinline__ void fill(char* smem, const Ctx& c, int wave) {
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int i = 0; i < NLOAD; ++i) issue_one(c, (uint32_t)(uintptr_t)smem + (uint32_t)(j * STAGE), j, i, wave);
+    }
+    static __device__ __forceinline__ i32x8 frag(const char* p, const char* q) {
+        const i32x4 lo = __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4*>(p)), hi = __builtin_bit_cast(i32x4, *reinterpret_cast<const u32x4*>(q));
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
-    static __device__ __forceinline__ void add(f32x4& acc, f32x4 part, f32x4 s) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r] = __builtin_fmaf(part[r], s[r], acc[r]);
+    struct Frags {
+        i32x8 a[HT], b[2];
+        f32x4 sw[BLOCK == 1 ? HT : 1];
+        float sw0, s[2];
+    };
+    // what a step starts with: the columns' fragments and scales, and the first 16 rows'
+    static __device__ __forceinline__ void read_a(const char* stage, const Ctx& c, Frags& f, int ht) {
+        f.a[ht] = frag(stage + c.rdw + 2048 * ht, stage + (c.rdw ^ 64u) + 2048 * ht);
+        if (BLOCK == 1) f.sw[BLOCK == 1 ? ht : 0] = *reinterpret_cast<const f32x4*>(stage + c.sw + 64 * ht);
+        else if (ht == 0) f.sw0 = *reinterpret_cast<const float*>(stage + c.sw);
     }
-    static __device__ __forceinline__ void step(const char* stage, const Ctx& c, f32x4 (&acc)[HT][MT]) {
+    static __device__ __forceinline__ void read_b(const char* stage, const Ctx& c, Frags& f, int mt) {
+        f.b[mt & 1] = frag(stage + c.rdx + 2048 * mt, stage + (c.rdx ^ 64u) + 2048 * mt);
+        f.s[mt & 1] = *reinterpret_cast<const float*>(stage + c.sx + 64 * mt);
+    }
+    // filled: the first stages were issued before the epilogue of the item before, whose stores are younger
+    static __device__ __forceinline__ void run(char* smem, const Ctx& c, f32x4 (&acc)[HT][MT], int wave, bool filled) {
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        i32x8 a[HT];
-        f32x4 sw[HT];
-#pragma unroll
-        for (int ht = 0; ht < HT; ++ht) {
-            a[ht] = frag(stage, c.rdw[ht]);
-            if (BLOCK == 1) sw[ht] = __builtin_bit_cast(f32x4, *reinterpret_cast<const u32x4*>(stage + c.sw + 64 * ht));
-        }
-        const float sw0 = BLOCK == 1 ? 1.0f : *reinterpret_cast<const float*>(stage + c.sw);
-        f32x4 part[2][HT];
-        float s[2];
-#pragma unroll
-        for (int mt = 0; mt <= MT; ++mt) {
-            if (mt < MT) {
-                const i32x8 b = frag(stage, c.rdx[mt]);
-                s[mt & 1] = *reinterpret_cast<const float*>(stage + c.sx + 64 * mt) * sw0;
-#pragma unroll
-                for (int ht = 0; ht < HT; ++ht) part[mt & 1][ht] = mma_e4m3(a[ht], b, zero);
-            }
-            if (mt > 0) {
-                const float f = s[(mt - 1) & 1];
-#pragma unroll
-                for (int ht = 0; ht < HT; ++ht)
-                    add(acc[ht][mt - 1], part[(mt - 1) & 1][ht], BLOCK == 1 ? sw[ht] * f : f32x4{f, f, f, f});
-            }
-        }
-    }
-    static __device__ __forceinline__ void run(char* smem, const Ctx& c, f32x4 (&acc)[HT][MT], int tid) {
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) acc[ht][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int mt = 0; mt < MT; ++mt) acc[ht][mt] = zero;
         const int KT = (c.K + 127) / 128;
         const uint32_t lds = (uint32_t)(uintptr_t)smem;
+        if (filled) lds_loads_in_flight_at_most<(NS - 1) * NLOAD + STORES>();
+        else lds_loads_in_flight_at_most<(NS - 1) * NLOAD>();
+        __syncthreads();
+        Frags f;
+        f32x4 part[LAG];
+        read_b(smem, c, f, 0);
 #pragma unroll
-        for (int j = 0; j < NS - 1; ++j)
-            if (j < KT) issue(c, lds + (uint32_t)(j * STAGE), j, tid);
+        for (int ht = 0; ht < HT; ++ht) read_a(smem, c, f, ht);
         int slot = 0;
         for (int s = 0; s < KT; ++s) {
-            // this step's stage has landed; everybody is done with the one before, whose place the next loads take
-            if (s + NS - 1 <= KT) lds_loads_in_flight_at_most<(NS - 2) * NLOAD>();
-            else lds_loads_in_flight_at_most<0>();
-            __syncthreads();
-            if (s + NS - 1 < KT) issue(c, lds + (uint32_t)((slot == 0 ? NS - 1 : slot - 1) * STAGE), s + NS - 1, tid);
-            step(smem + slot * STAGE, c, acc);
+            const char* cur = smem + slot * STAGE;
+            const uint32_t ld = lds + (uint32_t)(slot * STAGE);
             slot = slot == NS - 1 ? 0 : slot + 1;
+            const char* nxt = smem + slot * STAGE;
+            f32x4 sw[HT];     // this step's column scales: the last multiply-adds run after the next ones are read
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) sw[ht] = BLOCK == 1 ? f.sw[BLOCK == 1 ? ht : 0] : f32x4{f.sw0, f.sw0, f.sw0, f.sw0};
+            float row[2];
+            // MFMA i: rows i / HT, columns i % HT; the multiply-adds of part j beside it
+            auto add = [&](int j) {
+                const int mt = j / HT, ht = j % HT;
+                if (BLOCK == 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[ht][mt][r] = __builtin_fmaf(part[j % LAG][r], sw[ht][r] * row[mt & 1], acc[ht][mt][r]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[ht][mt][r] = __builtin_fmaf(part[j % LAG][r], row[mt & 1], acc[ht][mt][r]);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < NM; ++i) {
+                const int mt = i / HT, ht = i % HT;
+                if (i >= LAG) add(i - LAG);
+                if (ht == 0) {
+                    row[mt & 1] = BLOCK == 1 ? f.s[mt & 1] : f.s[mt & 1] * sw[0][0];
+                    if (mt + 1 < MT) read_b(cur, c, f, mt + 1);
+                    if (mt == MT - 1) {
+                        lds_loads_in_flight_at_most<(NS - 2) * NLOAD>();
+                        __syncthreads();
+                    }
+                }
+                part[i % LAG] = mma_e4m3(f.a[ht], f.b[mt & 1], zero);
+                if (mt == MT - 1) {
+                    if (ht == 0) read_b(nxt, c, f, 0);
+                    read_a(nxt, c, f, ht);
+#pragma unroll
+                    for (int e = (ht * NLOAD) / HT; e < ((ht + 1) * NLOAD) / HT; ++e) issue_one(c, ld, s + NS, e, wave);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = NM - LAG; j < NM; ++j) add(j);
         }
-        __syncthreads();   // LDS is the caller's
+        __syncthreads();   // the stages are the next item's
     }
-    // Y: the tile's first row and column; through LDS, 16 rows at a time, so that a row's part of the tile is stored in whole lines
-    static __device__ __forceinline__ void store(char* smem, const f32x4 (&acc)[HT][MT], char* Y, int64_t ldy, int have_m, int have_n, int tid) {
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    // Y: the tile's first row and column; through LDS of its own, 16 rows at a time, so that a row's part of the tile is stored in
+    // whole lines.  Every wave issues STORES stores, those past the tile's rows and columns out of range.
+    static __device__ __forceinline__ void store(char* smem, const f32x4 (&acc)[HT][MT], char* Y, uint32_t ldy, int have_m, int have_n, int wave) {
+        int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
+        asm volatile("" : "+v"(lane));   // (otherwise the addresses below are computed before the main loop and kept through it)
         const int wm = wave % WM, wn = wave / WM;
         const uint32_t x = lane & 15, g = lane >> 4;
-        char* mine = smem + wave * 16 * ROW;
-        constexpr int LPR = ROW / 16, RPI = 64 / LPR;   // lanes a row and rows an instruction on the way out
+        char* mine = smem + EPI + wave * 16 * ROW;
         const uint32_t rin = lane / LPR, ch = lane % LPR;
         const int col = wn * WNR + 8 * (int)ch;
+        const __amdgpu_buffer_rsrc_t ry = make_rsrc(Y, (uint32_t)min(have_m, BM) * 2u * ldy);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
             const uint32_t key = (x >> (ROW == 128 ? 1 : 2)) & (SLOTS - 1);
@@ -200,7 +233,7 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
                 u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + ((ch ^ (k >> 1)) << 4));
                 if (k & 1u) v = u32x4{v[2], v[3], v[0], v[1]};
                 const int m = wm * WMR + 16 * mt + (int)row;
-                if (m < have_m && col < have_n) *reinterpret_cast<u32x4*>(Y + (m * ldy + col) * 2) = v;
+                __builtin_amdgcn_raw_buffer_store_b128(v, ry, m < have_m && col < have_n ? ((uint32_t)m * ldy + (uint32_t)col) * 2u : kOob, 0, 0);
             }
         }
     }
@@ -209,25 +242,37 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
 template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK>
 __global__ __launch_bounds__(64 * WM * WN) void fp8_product_kernel(Fp8Args a) {
     typedef Fp8Gemm<T, BM, BN, WM, WN, NS, BLOCK> G;
+    static_assert(G::LDS_BYTES <= kLdsBesideGroups, "LDS");
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     extern __shared__ __attribute__((aligned(16))) char table[];
-    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3;
+    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Groups groups;
-    scan_groups(groups, table, a.offsets, a.E, a.R, BM, tid);
+    scan_groups(groups, table, smem, a.offsets, a.E, a.R, BM, tid);
     f32x4 acc[G::HT][G::MT];
     typename G::Ctx c;
     G::init_lds(c, tid);
     const int ncol = (a.N + BN - 1) / BN, KB = (a.K + 127) / 128, NB = (a.N + BLOCK - 1) / BLOCK;
-    GroupItem it;
-    for (int idx = blockIdx.x >> 3; group_item(groups, BM, ncol, xcd, idx, it); idx += step) {
+    GroupItem it, next;
+    int idx = blockIdx.x >> 3;
+    bool have = group_item(groups, BM, ncol, xcd, idx, it), filled = false;
+    auto aim = [&](const GroupItem& i) {
+        const int n0 = i.col * BN;
+        G::aim(c, static_cast<const char*>(a.A) + i.row0 * a.K, a.sa + i.row0, a.R, i.rows,
+               static_cast<const char*>(a.B) + ((int64_t)i.e * a.N + n0) * a.K, a.sb + (int64_t)i.e * KB * NB + n0 / BLOCK, NB, a.N - n0, a.K, tid);
+        G::fill(smem, c, wave);
+    };
+    if (have) aim(it);
+    while (have) {
+        G::run(smem, c, acc, wave, filled);
+        idx += step;
+        have = group_item(groups, BM, ncol, xcd, idx, next);
+        if (have) aim(next);
+        filled = true;
         const int n0 = it.col * BN;
-        G::aim(c, static_cast<const char*>(a.A) + it.row0 * a.K, a.sa + it.row0, a.R, it.rows,
-               static_cast<const char*>(a.B) + ((int64_t)it.e * a.N + n0) * a.K, a.sb + (int64_t)it.e * KB * NB + n0 / BLOCK, NB, a.N - n0, a.K, tid);
-        G::run(smem, c, acc, tid);
-        G::store(smem, acc, static_cast<char*>(a.Y) + (it.row0 * a.N + n0) * 2, a.N, it.rows, a.N - n0, tid);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+        G::store(smem, acc, static_cast<char*>(a.Y) + (it.row0 * a.N + n0) * 2, (uint32_t)a.N, it.rows, a.N - n0, wave);
+        it = next;
     }
+    lds_loads_in_flight_at_most<0>();   // (the last steps' loads write to LDS, if only zeros: not after the workgroup is gone)
 }
 
 // ---- quantising -------------------------------------------------------------------------------------------------
@@ -367,8 +412,18 @@ template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t 
     else hipLaunchKernelGGL((fp8_product_kernel<T, BM, BN, WM, WN, NS, 128>), grid, threads, group_table_bytes(a.E), st, a);
     return hipGetLastError();
 }
+// Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
+static constexpr Tile kFp8[] = {{256, 256, 1, 1.70f, 2.0f}, {128, 256, 1, 0.98f, 2.0f}, {128, 128, 1, 0.58f, 2.0f},
+                                {64, 128, 1, 0.37f, 1.5f}, {32, 128, 1, 0.31f, 1.5f}, {64, 64, 2, 0.43f, 1.5f}};
 template <typename T> static hipError_t product_any(const Fp8Args& a, int cus, hipStream_t st) {
-    return product<T, 128, 128, 2, 2, 4>(a, cus, 1, st);
+    switch (pick_tile(kFp8, a.R, a.E, a.N, a.K, cus)) {
+        case 0: return product<T, 256, 256, 2, 4, 2>(a, cus, 1, st);
+        case 1: return product<T, 128, 256, 2, 4, 2>(a, cus, 1, st);
+        case 2: return product<T, 128, 128, 4, 2, 4>(a, cus, 1, st);
+        case 3: return product<T, 64, 128, 2, 4, 5>(a, cus, 1, st);
+        case 4: return product<T, 32, 128, 1, 4, 6>(a, cus, 1, st);
+        default: return product<T, 64, 64, 2, 2, 4>(a, cus, 2, st);
+    }
 }
 hipError_t launch_fp8_product(int dtype, const Fp8Args& a, int cus, hipStream_t st) {
     return dtype == 0 ? product_any<__bf16>(a, cus, st) : product_any<_Float16>(a, cus, st);

@@ -7,67 +7,52 @@
 // The boundaries of the groups are on the device (ffuse_groups.h), so the host knows neither how many row blocks
 // there are nor whose they are: forward and input run persistent workgroups, which each lay the row blocks of all
 // groups end to end and take their share; a weight gradient's blocks are known beforehand.
-#include "ffuse_gemm2.h"
 #include "ffuse_gemm3.h"
 #include "ffuse_groups.h"
 #include "ffuse_launch.h"
 
 namespace ffuse {
 
-// ---- forward ----------------------------------------------------------------------------------------------------
-template <typename T, typename G, int BM, int BH, int THREADS>
-__global__ __launch_bounds__(THREADS) void grouped_forward_kernel(GroupedArgs a) {
+// ---- forward, and the gradient of the input -------------------------------------------------------------------------
+// The rows of each group times its matrix, or its transpose: persistent workgroups; an item's first loads go out
+// before the epilogue of the one before.  BCOL: Y = act(A W) (.* A W3), W [E][K][N]; otherwise Y = A W^T, W [E][N][K].
+template <typename T, bool BCOL, bool GATED, int BM, int BN, int WM, int WN, int NS>
+__global__ __launch_bounds__(64 * WM * WN) void grouped_rows_kernel(GroupedArgs a) {
+    typedef PairGemm<T, false, BCOL, GATED, BM, BN, WM, WN, NS> G;
+    static_assert(G::LDS_BYTES <= kLdsBesideGroups, "LDS");
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
     extern __shared__ __attribute__((aligned(16))) char table[];
-    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3;
+    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     Groups groups;
-    scan_groups(groups, table, a.offsets, a.E, a.R, BM, tid);
-    f32x16 acc[G::HT][G::MT], acc3[G::G == 2 ? G::HT : 1][G::G == 2 ? G::MT : 1];
+    scan_groups(groups, table, smem, a.offsets, a.E, a.R, BM, tid);
+    f32x4 acc[G::G][G::HT][G::MT];
     typename G::Ctx c;
-    G::init_lds(c, tid);
-    const int ncol = (a.N + BH - 1) / BH;
-    const int64_t wbytes = 2 * (int64_t)a.K * a.N;
-    GroupItem it;
-    for (int idx = blockIdx.x >> 3; group_item(groups, BM, ncol, xcd, idx, it); idx += step) {
-        const int rows = min(it.rows, BM);
-        const char* X = static_cast<const char*>(a.A) + it.row0 * a.K * 2;
-        const char* W = static_cast<const char*>(a.W) + it.e * wbytes;
-        const char* W3 = G::G == 2 ? static_cast<const char*>(a.W3) + it.e * wbytes : nullptr;
-        G::init_a(c, X, (uint32_t)rows * (uint32_t)(2 * a.K), 0u, 0u, (uint32_t)a.K, a.K, tid);
-        G::init_b(c, W, W3, (uint32_t)wbytes, (uint32_t)a.N, (uint32_t)a.N, (uint32_t)(it.col * BH), tid);
-        G::run(smem, c, 0, a.K, acc, acc3, tid);
-        char* Y = static_cast<char*>(a.C) + it.row0 * a.N * 2;
-        if constexpr (BM == 256) G::store_tile_slabs_rt(smem, a.act, acc, acc3, Y, a.N, 0, it.col * BH, rows, a.N, __builtin_amdgcn_readfirstlane(tid >> 6));
-        else G::store_tile_lds_rt(smem, a.act, acc, acc3, Y, a.N, 0, it.col * BH, rows, a.N, tid);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+    G::init(c, wave, lane);
+    const int K = c.K = BCOL ? a.K : a.N, N = BCOL ? a.N : a.K, ncol = (N + BN - 1) / BN;
+    GroupItem it, next;
+    int idx = blockIdx.x >> 3;
+    bool have = group_item(groups, BM, ncol, xcd, idx, it), filled = false;
+    auto aim = [&](const GroupItem& i) {
+        const int n0 = i.col * BN;
+        c.a.aim(static_cast<const char*>(a.A) + i.row0 * K * 2, K, i.rows, K, wave, lane);
+        const int64_t w = ((int64_t)i.e * K * N + (BCOL ? n0 : (int64_t)n0 * K)) * 2;
+        c.b[0].aim(static_cast<const char*>(a.W) + w, BCOL ? N : K, N - n0, K, wave, lane);
+        if (GATED) c.b[G::G - 1].aim(static_cast<const char*>(a.W3) + w, BCOL ? N : K, N - n0, K, wave, lane);
+        G::fill(smem, c);
+    };
+    if (have) aim(it);
+    while (have) {
+        G::run(smem, c, acc, filled);
+        idx += step;
+        have = group_item(groups, BM, ncol, xcd, idx, next);
+        if (have) aim(next);
+        filled = true;
+        char* Y = static_cast<char*>(a.C) + (it.row0 * N + it.col * BN) * 2;
+        if (BCOL) G::store_rt(smem, a.act, acc, Y, (uint32_t)N, it.rows, N - it.col * BN, wave);
+        else G::template store<ACT_IDENTITY>(smem, acc, Y, (uint32_t)N, it.rows, N - it.col * BN, wave);
+        it = next;
     }
-}
-
-// ---- gradient of the input --------------------------------------------------------------------------------------
-template <typename T, int BM, int BN, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN) void grouped_input_kernel(GroupedArgs a) {
-    typedef RowGemm<T, BM, BN, WM, WN, NS> G;
-    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
-    extern __shared__ __attribute__((aligned(16))) char table[];
-    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3;
-    Groups groups;
-    scan_groups(groups, table, a.offsets, a.E, a.R, BM, tid);
-    f32x16 acc[G::HT][G::MT], none[1][1];
-    typename G::Ctx c;
-    G::init_lds(c, tid);
-    const int ncol = (a.K + BN - 1) / BN;
-    GroupItem it;
-    for (int idx = blockIdx.x >> 3; group_item(groups, BM, ncol, xcd, idx, it); idx += step) {
-        const int col0 = it.col * BN;
-        G::aim(c, static_cast<const char*>(a.A) + it.row0 * a.N * 2, it.rows,
-               static_cast<const char*>(a.W) + ((int64_t)it.e * a.K + col0) * a.N * 2, a.K - col0, a.N, tid);
-        G::run(smem, c, acc);
-        char* dX = static_cast<char*>(a.C) + it.row0 * a.K * 2;
-        G::template store_tile_lds<ACT_IDENTITY>(smem, acc, none, dX, a.K, 0, col0, min(it.rows, BM), a.K, tid);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    }
+    lds_loads_in_flight_at_most<0>();   // (the last steps' loads write to LDS, if only zeros: not after the workgroup is gone)
 }
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------
@@ -75,50 +60,69 @@ __global__ __launch_bounds__(64 * WM * WN) void grouped_input_kernel(GroupedArgs
 // free, which evens out groups of different lengths.
 template <typename T, int BM, int BN, int WM, int WN, int NS>
 __global__ __launch_bounds__(64 * WM * WN) void grouped_weights_kernel(GroupedArgs a) {
-    typedef ColGemm<T, BM, BN, WM, WN, NS> G;
+    typedef PairGemm<T, true, true, false, BM, BN, WM, WN, NS> G;
     __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int mb = (a.K + BM - 1) / BM, nb = (a.N + BN - 1) / BN;
     const int e = (int)(blockIdx.x / (uint32_t)(mb * nb)), b = (int)(blockIdx.x % (uint32_t)(mb * nb));
     // (any boundaries are taken: the rows read are inside the tensor, and nothing but dW[e] is written)
     const int first = min(max(a.offsets[e], 0), a.R), last = min(max(a.offsets[e + 1], 0), a.R);
-    const int rows = max(last - first, 0);
     const int band = b / (kGroupBand * nb), in = b - band * kGroupBand * nb, h = min(kGroupBand, mb - band * kGroupBand);
     const int m0 = (band * kGroupBand + in % h) * BM, n0 = in / h * BN;
-    f32x16 acc[G::HT][G::MT], none[1][1];
+    f32x4 acc[G::G][G::HT][G::MT];
     typename G::Ctx c;
-    G::init_lds(c, tid);
-    G::aim(c, static_cast<const char*>(a.A) + ((int64_t)first * a.K + m0) * 2, a.K, a.K - m0,
-           static_cast<const char*>(a.W) + ((int64_t)first * a.N + n0) * 2, a.N, a.N - n0, rows, tid);
-    G::run(smem, c, acc);
-    char* dW = static_cast<char*>(a.C) + (int64_t)e * a.K * a.N * 2;
-    G::template store_tile_lds<ACT_IDENTITY>(smem, acc, none, dW, a.N, m0, n0, a.K, a.N, tid);
+    G::init(c, wave, lane);
+    c.K = max(last - first, 0);
+    c.a.aim(static_cast<const char*>(a.A) + ((int64_t)first * a.K + m0) * 2, a.K, a.K - m0, c.K, wave, lane);
+    c.b[0].aim(static_cast<const char*>(a.W) + ((int64_t)first * a.N + n0) * 2, a.N, a.N - n0, c.K, wave, lane);
+    G::fill(smem, c);
+    G::run(smem, c, acc, false);
+    char* dW = static_cast<char*>(a.C) + ((int64_t)e * a.K * a.N + (int64_t)m0 * a.N + n0) * 2;
+    G::template store<ACT_IDENTITY>(smem, acc, dW, (uint32_t)a.N, a.K - m0, a.N - n0, wave);
+    lds_loads_in_flight_at_most<0>();   // (loads past the last stage write to LDS, if only zeros: not after the workgroup is gone)
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------
-template <typename T, typename G, int BM, int BH, int THREADS> static hipError_t forward(const GroupedArgs& a, int cus, int per_cu, hipStream_t st) {
-    const int grid = persistent_grid(most_row_blocks(a.R, a.E, BM) * ((a.N + BH - 1) / BH), cus, per_cu);
-    hipLaunchKernelGGL((grouped_forward_kernel<T, G, BM, BH, THREADS>), dim3(grid), dim3(THREADS), group_table_bytes(a.E), st, a);
+// Tiles, and their times for 64 k: 16384 rows in eight uneven groups, 4096 x 11008 gated, 11008 x 4096 plain, 4096 x 4096 for
+// the gradient of the input, whose operands need no transposing.  A wave's part is 128 x 64 of the largest (256 x 128 gated: 128 x 32
+// of either branch) and 32 x 32 of the small ones.
+static constexpr Tile kGated[] = {{256, 128, 1, 1.60f, 2.0f}, {128, 128, 1, 0.93f, 2.0f}, {64, 128, 1, 0.72f, 2.0f}, {32, 128, 1, 0.63f, 2.0f}, {64, 64, 2, 0.87f, 2.0f}};
+static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f}, {128, 256, 1, 0.92f, 2.0f}, {64, 256, 1, 0.67f, 2.0f},
+                                  {64, 128, 1, 0.44f, 2.0f}, {32, 128, 1, 0.37f, 2.0f}, {64, 64, 2, 0.72f, 2.0f}};
+static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f}, {128, 256, 1, 0.90f, 2.0f}, {64, 256, 1, 0.65f, 2.0f},
+                                  {64, 128, 1, 0.38f, 2.0f}, {32, 128, 1, 0.28f, 2.0f}, {64, 64, 2, 0.45f, 2.0f}};
+
+template <typename T, bool BCOL, bool GATED, int BM, int BN, int WM, int WN, int NS> static hipError_t rows(const GroupedArgs& a, int cus, int per_cu, hipStream_t st) {
+    const int N = BCOL ? a.N : a.K;
+    const int grid = persistent_grid(most_row_blocks(a.R, a.E, BM) * ((N + BN - 1) / BN), cus, per_cu);
+    hipLaunchKernelGGL((grouped_rows_kernel<T, BCOL, GATED, BM, BN, WM, WN, NS>), dim3(grid), dim3(64 * WM * WN), group_table_bytes(a.E), st, a);
     return hipGetLastError();
 }
-template <typename T> static hipError_t forward_any(const GroupedArgs& a, int cus, hipStream_t st) {
-    if (a.W3) return forward<T, WideGemm<T, true, 128, 128, 4, 2, 4>, 128, 128, 512>(a, cus, 1, st);
-    return forward<T, WideGemm<T, false, 128, 256, 2, 4, 4>, 128, 256, 512>(a, cus, 1, st);
+template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hipStream_t st) {
+    switch (pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus)) {
+        case 0: return rows<T, true, true, 256, 128, 2, 4, 2>(a, cus, 1, st);
+        case 1: return rows<T, true, true, 128, 128, 2, 4, 3>(a, cus, 1, st);
+        case 2: return rows<T, true, true, 64, 128, 2, 4, 3>(a, cus, 1, st);
+        case 3: return rows<T, true, true, 32, 128, 1, 4, 3>(a, cus, 1, st);
+        default: return rows<T, true, true, 64, 64, 2, 2, 3>(a, cus, 2, st);
+    }
+}
+template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, int cus, hipStream_t st) {
+    switch (BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus)) {
+        case 0: return rows<T, BCOL, false, 256, 256, 2, 4, 2>(a, cus, 1, st);
+        case 1: return rows<T, BCOL, false, 128, 256, 2, 4, 3>(a, cus, 1, st);
+        case 2: return rows<T, BCOL, false, 64, 256, 2, 4, 3>(a, cus, 1, st);
+        case 3: return rows<T, BCOL, false, 64, 128, 2, 4, 4>(a, cus, 1, st);
+        case 4: return rows<T, BCOL, false, 32, 128, 1, 4, 4>(a, cus, 1, st);
+        default: return rows<T, BCOL, false, 64, 64, 2, 2, 4>(a, cus, 2, st);
+    }
 }
 hipError_t launch_grouped_forward(int dtype, const GroupedArgs& a, int cus, hipStream_t st) {
-    return dtype == 0 ? forward_any<__bf16>(a, cus, st) : forward_any<_Float16>(a, cus, st);
-}
-
-template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t input(const GroupedArgs& a, int cus, int per_cu, hipStream_t st) {
-    const int grid = persistent_grid(most_row_blocks(a.R, a.E, BM) * ((a.K + BN - 1) / BN), cus, per_cu);
-    hipLaunchKernelGGL((grouped_input_kernel<T, BM, BN, WM, WN, NS>), dim3(grid), dim3(64 * WM * WN), group_table_bytes(a.E), st, a);
-    return hipGetLastError();
-}
-template <typename T> static hipError_t input_any(const GroupedArgs& a, int cus, hipStream_t st) {
-    return input<T, 128, 128, 2, 2, 4>(a, cus, 1, st);
+    if (a.W3) return dtype == 0 ? gated<__bf16>(a, cus, st) : gated<_Float16>(a, cus, st);
+    return dtype == 0 ? plain<__bf16, true>(a, cus, st) : plain<_Float16, true>(a, cus, st);
 }
 hipError_t launch_grouped_input(int dtype, const GroupedArgs& a, int cus, hipStream_t st) {
-    return dtype == 0 ? input_any<__bf16>(a, cus, st) : input_any<_Float16>(a, cus, st);
+    return dtype == 0 ? plain<__bf16, false>(a, cus, st) : plain<_Float16, false>(a, cus, st);
 }
 
 template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t weights(const GroupedArgs& a, hipStream_t st) {
@@ -126,11 +130,17 @@ template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t 
     hipLaunchKernelGGL((grouped_weights_kernel<T, BM, BN, WM, WN, NS>), dim3((unsigned)grid), dim3(64 * WM * WN), 0, st, a);
     return hipGetLastError();
 }
-template <typename T> static hipError_t weights_any(const GroupedArgs& a, hipStream_t st) {
-    return weights<T, 128, 128, 2, 2, 4>(a, st);
+// 256 x 256 takes 1.9 us for 64 rows, two of 128 x 128 side by side 1.2: four fill as many CUs twice as well, where there are few
+template <typename T> static hipError_t weights_any(const GroupedArgs& a, int cus, hipStream_t st) {
+    const auto items = [&](int b) { return (double)a.E * ((a.K + b - 1) / b) * ((a.N + b - 1) / b); };
+    const double steps = (double)a.R / a.E / 64, big = items(256) / cus, small = items(128) / (2 * cus);
+    const double t_big = (big <= 1.0 ? 1.0 : big + 0.3) * (4.0 + 1.9 * steps);
+    const double t_small = (small <= 1.0 ? 1.0 : small + 0.3) * (4.0 + 1.2 * (small <= 0.5 ? 0.6 : 1.0) * steps);
+    if (t_big <= t_small) return weights<T, 256, 256, 2, 4, 2>(a, st);
+    return weights<T, 128, 128, 2, 2, 2>(a, st);
 }
-hipError_t launch_grouped_weights(int dtype, const GroupedArgs& a, hipStream_t st) {
-    return dtype == 0 ? weights_any<__bf16>(a, st) : weights_any<_Float16>(a, st);
+hipError_t launch_grouped_weights(int dtype, const GroupedArgs& a, int cus, hipStream_t st) {
+    return dtype == 0 ? weights_any<__bf16>(a, cus, st) : weights_any<_Float16>(a, cus, st);
 }
 
 }  // namespace ffuse

@@ -89,7 +89,7 @@ int ffuse_grouped_gemm_dw(int dtype, const void* X, const void* dY, const int32_
     int cus = 0;
     const int rc = ffuse::device_ready(&cus);
     if (rc != FFUSE_OK) return rc;
-    return status(ffuse::launch_grouped_weights(dtype, grouped_args(X, dY, nullptr, offsets, dW, R, E, K, N, 0), static_cast<hipStream_t>(stream)));
+    return status(ffuse::launch_grouped_weights(dtype, grouped_args(X, dY, nullptr, offsets, dW, R, E, K, N, 0), cus, static_cast<hipStream_t>(stream)));
 }
 
 size_t ffuse_grouped_workspace_bytes(int dtype, int64_t R, int64_t N1) {

@@ -13,18 +13,21 @@ static constexpr int kMaxGroups = 1024;   // groups of a call: their boundaries 
 static constexpr int kGroupBand = 8;      // row blocks that share their column blocks in an XCD's L2 at a time
 
 // LDS bytes of the tables below
-__host__ __device__ inline int group_table_bytes(int E) { return 4 * (2 * E + 1); }
+__host__ __device__ constexpr int group_table_bytes(int E) { return 8 * E; }
+// LDS that the kernels' own arrays may take beside the largest tables (160 KB in all)
+static constexpr int kLdsBesideGroups = 160 * 1024 - group_table_bytes(kMaxGroups);
 
 struct Groups {
-    int* start;   // [E + 1]: the clamped boundaries
+    int* start;   // [E]: the clamped boundaries
     int* tiles;   // [E]: row blocks of the groups up to and including this one
-    int E;
+    int E, end;   // end: the last boundary
 };
 
 // Fills the tables; the whole workgroup calls it, the first wave works.  offsets == nullptr: one group of all R rows.
-__device__ __forceinline__ void scan_groups(Groups& g, char* table, const int32_t* offsets, int E, int R, int bm, int tid) {
+// scratch: 4 bytes of LDS that are free again afterwards.
+__device__ __forceinline__ void scan_groups(Groups& g, char* table, char* scratch, const int32_t* offsets, int E, int R, int bm, int tid) {
     g.start = reinterpret_cast<int*>(table);
-    g.tiles = g.start + E + 1;
+    g.tiles = g.start + E;
     g.E = E;
     if (tid < 64) {
         int most = 0, sum = 0;   // of the groups before this round of 64
@@ -53,12 +56,15 @@ __device__ __forceinline__ void scan_groups(Groups& g, char* table, const int32_
             if (live) {
                 g.start[e] = lo;
                 g.tiles[e] = n;
-                if (e == E - 1) g.start[E] = hi;
+                if (e == E - 1) *reinterpret_cast<int*>(scratch) = hi;
             }
             most = __shfl(lo, 63);
             sum = __shfl(n, 63);
         }
     }
+    __syncthreads();
+
+    g.end = __builtin_amdgcn_readfirstlane(*reinterpret_cast<int*>(scratch));
     __syncthreads();
 }
 
@@ -73,7 +79,7 @@ struct GroupItem {
 // column block by column block, so that the 32 workgroups of an XCD work on a patch of a band and a few column
 // blocks and fetch each panel of either operand into its L2 once.  ncol: column blocks.
 __device__ __forceinline__ bool group_item(const Groups& g, int bm, int ncol, int xcd, int idx, GroupItem& it) {
-    const int total = g.tiles[g.E - 1] * ncol;
+    const int total = __builtin_amdgcn_readfirstlane(g.tiles[g.E - 1]) * ncol;
     const int per = (total + 7) >> 3;
     const int v = xcd * per + idx;
     if (idx >= per || v >= total) return false;
@@ -90,7 +96,7 @@ __device__ __forceinline__ bool group_item(const Groups& g, int bm, int ncol, in
     const int w = v - t0 * ncol, band = w / (kGroupBand * ncol), in = w - band * kGroupBand * ncol;
     const int h = min(kGroupBand, nt - band * kGroupBand);
     const int c = in / h, r = band * kGroupBand + in - c * h;
-    const int first = __builtin_amdgcn_readfirstlane(g.start[e]), last = __builtin_amdgcn_readfirstlane(g.start[e + 1]);
+    const int first = __builtin_amdgcn_readfirstlane(g.start[e]), last = __builtin_amdgcn_readfirstlane(e + 1 < g.E ? g.start[e + 1] : g.end);
     it.e = e;
     it.row0 = (int64_t)first + (int64_t)r * bm;
     it.rows = last - first - r * bm;
@@ -109,6 +115,30 @@ inline int persistent_grid(int64_t items, int cus, int per_cu) {
     const int64_t most = (int64_t)cus * per_cu;
     const int64_t n = items < most ? items : most;
     return (int)((n + 7) / 8 * 8);
+}
+
+// A tile that a kernel is built for, and what an item of it takes: `step` us for each 128 bytes of the contraction, measured
+// with every CU at work on `per_cu` items of a large problem, and `fixed` us beside them.
+struct Tile {
+    int bm, bn, per_cu;
+    float step, fixed;
+};
+// The tile whose rounds of items take the least time.  Where the boundaries are known on the device alone, every group
+// is taken to have the average number of rows and half a block more.
+template <int N> int pick_tile(const Tile (&tiles)[N], int64_t R, int64_t E, int64_t cols, int64_t bytes, int cus) {
+    int best = 0;
+    double least = 0.0;
+    for (int i = 0; i < N; ++i) {
+        const Tile& t = tiles[i];
+        const double groups = (double)(R < E ? R : E), mean = R / groups;
+        const double blocks = E == 1 ? (double)((R + t.bm - 1) / t.bm) : mean <= 1.0 ? groups : groups * (mean / t.bm + 0.5 > 1.0 ? mean / t.bm + 0.5 : 1.0);
+        const double per_cu = blocks * (double)((cols + t.bn - 1) / t.bn) / cus, x = per_cu / t.per_cu;
+        const double rounds = x <= 1.0 ? 1.0 : E == 1 ? (double)(int64_t)(x + 0.999) : x + 0.5;
+        const double alone = per_cu <= 1.0 && t.per_cu > 1 ? 0.6 : 1.0;   // an item that has a CU to itself is done sooner
+        const double time = rounds * (t.fixed + t.step * alone * (double)((bytes + 127) / 128));
+        if (i == 0 || time < least) { best = i; least = time; }
+    }
+    return best;
 }
 
 }  // namespace ffuse

@@ -153,7 +153,7 @@ struct GroupedArgs {
 };
 hipError_t launch_grouped_forward(int dtype, const GroupedArgs& a, int cus, hipStream_t st);
 hipError_t launch_grouped_input(int dtype, const GroupedArgs& a, int cus, hipStream_t st);
-hipError_t launch_grouped_weights(int dtype, const GroupedArgs& a, hipStream_t st);
+hipError_t launch_grouped_weights(int dtype, const GroupedArgs& a, int cus, hipStream_t st);
 
 // products in e4m3 with a scale per block of 128 along the contraction (ffuse_fp8.hip)
 struct Fp8Args {
