@@ -435,29 +435,38 @@ def ffuse_conv_chain_f16(X, W1, W2, act, Y, stream=None, check=True):
 
 
 # ---- products grouped by expert, and 8-bit products.  Sizes come from the tensors, which are checked here: what the C ABI
-# sees of a tensor is an address.
+# sees of a tensor is an address.  (A single token's call lasts no longer on the device than a call takes here: each check is
+# an attribute or two.)
 
-def _want(name, t, shape, dtype):
+_torch = None
+_has_device = False
+
+
+def _tensors(dtype):
+    """torch, the operands' type and the current device."""
+    global _torch, _has_device
+    if _torch is None:
+        import torch
+        _has_device = torch.cuda.is_available()
+        _torch = torch
+    if dtype != DT_BF16 and dtype != DT_F16:
+        raise ValueError(f"dtype {dtype}: DT_BF16 or DT_F16")
+    return _torch, _torch.bfloat16 if dtype == DT_BF16 else _torch.float16, _torch.cuda.current_device() if _has_device else -2
+
+
+def _want(device, name, t, shape, dtype):
     """Raises unless t is a contiguous tensor of this shape and type on the current device."""
-    import torch
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} is needed, not {t.dtype} {tuple(t.shape)}"
                          f"{'' if t.is_contiguous() else ', not contiguous'}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != device:
         raise ValueError(f"{name}: on {t.device}, not on the current device")
 
 
-def _operand_dtype(dtype):
-    import torch
-    t = {DT_BF16: torch.bfloat16, DT_F16: torch.float16}.get(int(dtype))
-    if t is None:
-        raise ValueError(f"dtype {dtype}: DT_BF16 or DT_F16")
-    return t
-
-
-def _want_dims(name, t, n):
+def _sizes(name, t, n):
     if t.dim() != n:
         raise ValueError(f"{name}: {n} dimensions are needed, not {t.dim()}")
+    return t.shape
 
 
 def _rc(name, rc, check):
@@ -470,43 +479,40 @@ def ffuse_grouped_gemm(dtype, X, W, W3, offsets, act, Y, stream=None, check=True
     """Y[r] = act(X[r] W[e]) (.* X[r] W3[e]) for the rows r = offsets[e] .. offsets[e + 1] - 1 of each expert e.
 
     X [R][K], W and W3 (or None) [E][K][N], offsets [E + 1] int32, all on the device; Y [R][N] (rows of no group are left as they are)."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("X", X, 2)
-    _want_dims("W", W, 3)
-    (R, K), (E, _, N) = X.shape, W.shape
-    for name, x, shape, kind in (("X", X, (R, K), t), ("W", W, (E, K, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("Y", Y, (R, N), t)):
-        _want(name, x, shape, kind)
+    torch, t, dev = _tensors(dtype)
+    (R, K), (E, _, N) = _sizes("X", X, 2), _sizes("W", W, 3)
+    _want(dev, "X", X, (R, K), t)
+    _want(dev, "W", W, (E, K, N), t)
     if W3 is not None:
-        _want("W3", W3, (E, K, N), t)
-    return _rc("ffuse_grouped_gemm", lib().ffuse_grouped_gemm(int(dtype), _addr(X), _addr(W), _addr(W3), _addr(offsets), int(act), R, E, K, N, _addr(Y),
-                                                              _stream_addr(stream)), check)
+        _want(dev, "W3", W3, (E, K, N), t)
+    _want(dev, "offsets", offsets, (E + 1,), torch.int32)
+    _want(dev, "Y", Y, (R, N), t)
+    return _rc("ffuse_grouped_gemm", (_lib or lib()).ffuse_grouped_gemm(dtype, X.data_ptr(), W.data_ptr(), _addr(W3), offsets.data_ptr(), int(act), R, E, K, N,
+                                                                        Y.data_ptr(), _stream_addr(stream)), check)
 
 
 def ffuse_grouped_gemm_dx(dtype, dY, W, offsets, dX, stream=None, check=True):
     """dX[r] = dY[r] W[e]^T: the gradient of the plain product's input.  dY [R][N], W [E][K][N], dX [R][K]."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("dY", dY, 2)
-    _want_dims("W", W, 3)
-    (R, N), (E, K, _) = dY.shape, W.shape
-    for name, x, shape, kind in (("dY", dY, (R, N), t), ("W", W, (E, K, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("dX", dX, (R, K), t)):
-        _want(name, x, shape, kind)
-    return _rc("ffuse_grouped_gemm_dx", lib().ffuse_grouped_gemm_dx(int(dtype), _addr(dY), _addr(W), _addr(offsets), R, E, K, N, _addr(dX),
-                                                                    _stream_addr(stream)), check)
+    torch, t, dev = _tensors(dtype)
+    (R, N), (E, K, _) = _sizes("dY", dY, 2), _sizes("W", W, 3)
+    _want(dev, "dY", dY, (R, N), t)
+    _want(dev, "W", W, (E, K, N), t)
+    _want(dev, "offsets", offsets, (E + 1,), torch.int32)
+    _want(dev, "dX", dX, (R, K), t)
+    return _rc("ffuse_grouped_gemm_dx", (_lib or lib()).ffuse_grouped_gemm_dx(dtype, dY.data_ptr(), W.data_ptr(), offsets.data_ptr(), R, E, K, N, dX.data_ptr(),
+                                                                              _stream_addr(stream)), check)
 
 
 def ffuse_grouped_gemm_dw(dtype, X, dY, offsets, dW, stream=None, check=True):
     """dW[e] = X_e^T dY_e: the gradient of the plain product's weights, zeros for an expert without rows.  X [R][K], dY [R][N], dW [E][K][N]."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("X", X, 2)
-    _want_dims("dW", dW, 3)
-    (R, K), (E, _, N) = X.shape, dW.shape
-    for name, x, shape, kind in (("X", X, (R, K), t), ("dY", dY, (R, N), t), ("offsets", offsets, (E + 1,), torch.int32), ("dW", dW, (E, K, N), t)):
-        _want(name, x, shape, kind)
-    return _rc("ffuse_grouped_gemm_dw", lib().ffuse_grouped_gemm_dw(int(dtype), _addr(X), _addr(dY), _addr(offsets), R, E, K, N, _addr(dW),
-                                                                    _stream_addr(stream)), check)
+    torch, t, dev = _tensors(dtype)
+    (R, K), (E, _, N) = _sizes("X", X, 2), _sizes("dW", dW, 3)
+    _want(dev, "X", X, (R, K), t)
+    _want(dev, "dY", dY, (R, N), t)
+    _want(dev, "offsets", offsets, (E + 1,), torch.int32)
+    _want(dev, "dW", dW, (E, K, N), t)
+    return _rc("ffuse_grouped_gemm_dw", (_lib or lib()).ffuse_grouped_gemm_dw(dtype, X.data_ptr(), dY.data_ptr(), offsets.data_ptr(), R, E, K, N, dW.data_ptr(),
+                                                                              _stream_addr(stream)), check)
 
 
 def ffuse_grouped_workspace_bytes(dtype, R, N1) -> int:
@@ -515,83 +521,76 @@ def ffuse_grouped_workspace_bytes(dtype, R, N1) -> int:
 
 def ffuse_grouped_ffn(dtype, X, W1, W3, W2, offsets, act, Y, workspace, stream=None, check=True):
     """Y[r] = (act(X[r] W1[e]) (.* X[r] W3[e])) W2[e], the chain by expert.  W1, W3 (or None) [E][K][N1], W2 [E][N1][N2];
-    workspace: a device tensor of ffuse_grouped_workspace_bytes(dtype, R, N1) bytes."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("X", X, 2)
-    _want_dims("W2", W2, 3)
-    (R, K), (E, N1, N2) = X.shape, W2.shape
-    for name, x, shape, kind in (("X", X, (R, K), t), ("W1", W1, (E, K, N1), t), ("W2", W2, (E, N1, N2), t), ("offsets", offsets, (E + 1,), torch.int32),
-                                 ("Y", Y, (R, N2), t)):
-        _want(name, x, shape, kind)
+    workspace: a device tensor of ffuse_grouped_workspace_bytes(dtype, R, N1) bytes (None where there are no rows)."""
+    torch, t, dev = _tensors(dtype)
+    (R, K), (E, N1, N2) = _sizes("X", X, 2), _sizes("W2", W2, 3)
+    _want(dev, "X", X, (R, K), t)
+    _want(dev, "W1", W1, (E, K, N1), t)
     if W3 is not None:
-        _want("W3", W3, (E, K, N1), t)
+        _want(dev, "W3", W3, (E, K, N1), t)
+    _want(dev, "W2", W2, (E, N1, N2), t)
+    _want(dev, "offsets", offsets, (E + 1,), torch.int32)
+    _want(dev, "Y", Y, (R, N2), t)
     nbytes = 0
     if workspace is not None:
-        _want("workspace", workspace, workspace.shape, workspace.dtype)
+        _want(dev, "workspace", workspace, workspace.shape, workspace.dtype)
         nbytes = workspace.numel() * workspace.element_size()
-    return _rc("ffuse_grouped_ffn", lib().ffuse_grouped_ffn(int(dtype), _addr(X), _addr(W1), _addr(W3), _addr(W2), _addr(offsets), int(act), R, E, K, N1, N2,
-                                                            _addr(Y), _addr(workspace), nbytes, _stream_addr(stream)), check)
+    return _rc("ffuse_grouped_ffn", (_lib or lib()).ffuse_grouped_ffn(dtype, X.data_ptr(), W1.data_ptr(), _addr(W3), W2.data_ptr(), offsets.data_ptr(), int(act),
+                                                                      R, E, K, N1, N2, Y.data_ptr(), _addr(workspace), nbytes, _stream_addr(stream)), check)
 
 
 def ffuse_fp8_quantize(dtype, X, Q, scale, block_rows=1, transpose=False, stream=None, check=True):
     """X [M][K] as e4m3 numbers Q [M][K rounded up to 16] and fp32 scales [ceil(K / 128)][ceil(M / block_rows)], one for
     each block of block_rows (1 or 128) x 128; with transpose the same of X^T."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("X", X, 2)
-    M, K = X.shape
+    torch, t, dev = _tensors(dtype)
+    M, K = _sizes("X", X, 2)
     m, k = (K, M) if transpose else (M, K)
-    rows = 128 if block_rows == 128 else 1
-    for name, x, shape, kind in (("X", X, (M, K), t), ("Q", Q, (m, (k + 15) // 16 * 16), torch.float8_e4m3fn),
-                                 ("scale", scale, ((k + 127) // 128, (m + rows - 1) // rows), torch.float32)):
-        _want(name, x, shape, kind)
-    return _rc("ffuse_fp8_quantize", lib().ffuse_fp8_quantize(int(dtype), _addr(X), M, K, int(block_rows), int(bool(transpose)), _addr(Q), _addr(scale),
-                                                              _stream_addr(stream)), check)
+    _want(dev, "X", X, (M, K), t)
+    _want(dev, "Q", Q, (m, (k + 15) // 16 * 16), torch.float8_e4m3fn)
+    _want(dev, "scale", scale, ((k + 127) // 128, (m + 127) // 128 if block_rows == 128 else m), torch.float32)
+    return _rc("ffuse_fp8_quantize", (_lib or lib()).ffuse_fp8_quantize(dtype, X.data_ptr(), M, K, int(block_rows), 1 if transpose else 0, Q.data_ptr(),
+                                                                        scale.data_ptr(), _stream_addr(stream)), check)
 
 
 def _fp8_block(sb, kb, N):
     """1 or 128: the rows of B that share a scale, from the shape of the scales."""
+    last = sb.shape[-2:]
     for block in (128, 1):
-        if tuple(sb.shape[-2:]) == (kb, (N + block - 1) // block):
+        if last == (kb, (N + block - 1) // block):
             return block
-    raise ValueError(f"scales of B: the last dimensions are needed as {(kb, (N + 127) // 128)} or {(kb, N)}, not {tuple(sb.shape[-2:])}")
+    raise ValueError(f"scales of B: the last dimensions are needed as {(kb, (N + 127) // 128)} or {(kb, N)}, not {tuple(last)}")
 
 
 def ffuse_gemm_fp8(dtype, A, sa, B, sb, Y, stream=None, check=True):
     """Y [M][N] (DT_BF16 or DT_F16) = the product of A [M][K] and B [N][K], both e4m3, sa [ceil(K / 128)][M] and sb
     [ceil(K / 128)][ceil(N / 128) or N] their scales."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("A", A, 2)
-    _want_dims("B", B, 2)
-    (M, K), (N, _) = A.shape, B.shape
+    torch, t, dev = _tensors(dtype)
+    (M, K), (N, _) = _sizes("A", A, 2), _sizes("B", B, 2)
     kb = (K + 127) // 128
     block = _fp8_block(sb, kb, N)
-    e4m3, f32 = torch.float8_e4m3fn, torch.float32
-    for name, x, shape, kind in (("A", A, (M, K), e4m3), ("sa", sa, (kb, M), f32), ("B", B, (N, K), e4m3), ("sb", sb, (kb, (N + block - 1) // block), f32),
-                                 ("Y", Y, (M, N), t)):
-        _want(name, x, shape, kind)
-    return _rc("ffuse_gemm_fp8", lib().ffuse_gemm_fp8(int(dtype), _addr(A), _addr(sa), _addr(B), _addr(sb), block, M, K, N, _addr(Y), _stream_addr(stream)),
-               check)
+    _want(dev, "A", A, (M, K), torch.float8_e4m3fn)
+    _want(dev, "sa", sa, (kb, M), torch.float32)
+    _want(dev, "B", B, (N, K), torch.float8_e4m3fn)
+    _want(dev, "sb", sb, (kb, (N + block - 1) // block), torch.float32)
+    _want(dev, "Y", Y, (M, N), t)
+    return _rc("ffuse_gemm_fp8", (_lib or lib()).ffuse_gemm_fp8(dtype, A.data_ptr(), sa.data_ptr(), B.data_ptr(), sb.data_ptr(), block, M, K, N, Y.data_ptr(),
+                                                                _stream_addr(stream)), check)
 
 
 def ffuse_grouped_gemm_fp8(dtype, A, sa, B, sb, offsets, Y, stream=None, check=True):
     """ffuse_gemm_fp8 with the rows of A grouped by expert: B [E][N][K], sb [E][ceil(K / 128)][ceil(N / 128) or N]."""
-    import torch
-    t = _operand_dtype(dtype)
-    _want_dims("A", A, 2)
-    _want_dims("B", B, 3)
-    _want_dims("sb", sb, 3)
-    (R, K), (E, N, _) = A.shape, B.shape
+    torch, t, dev = _tensors(dtype)
+    (R, K), (E, N, _), _ = _sizes("A", A, 2), _sizes("B", B, 3), _sizes("sb", sb, 3)
     kb = (K + 127) // 128
     block = _fp8_block(sb, kb, N)
-    e4m3, f32 = torch.float8_e4m3fn, torch.float32
-    for name, x, shape, kind in (("A", A, (R, K), e4m3), ("sa", sa, (kb, R), f32), ("B", B, (E, N, K), e4m3),
-                                 ("sb", sb, (E, kb, (N + block - 1) // block), f32), ("offsets", offsets, (E + 1,), torch.int32), ("Y", Y, (R, N), t)):
-        _want(name, x, shape, kind)
-    return _rc("ffuse_grouped_gemm_fp8", lib().ffuse_grouped_gemm_fp8(int(dtype), _addr(A), _addr(sa), _addr(B), _addr(sb), block, _addr(offsets), R, E, K, N,
-                                                                      _addr(Y), _stream_addr(stream)), check)
+    _want(dev, "A", A, (R, K), torch.float8_e4m3fn)
+    _want(dev, "sa", sa, (kb, R), torch.float32)
+    _want(dev, "B", B, (E, N, K), torch.float8_e4m3fn)
+    _want(dev, "sb", sb, (E, kb, (N + block - 1) // block), torch.float32)
+    _want(dev, "offsets", offsets, (E + 1,), torch.int32)
+    _want(dev, "Y", Y, (R, N), t)
+    return _rc("ffuse_grouped_gemm_fp8", (_lib or lib()).ffuse_grouped_gemm_fp8(dtype, A.data_ptr(), sa.data_ptr(), B.data_ptr(), sb.data_ptr(), block,
+                                                                                offsets.data_ptr(), R, E, K, N, Y.data_ptr(), _stream_addr(stream)), check)
 
 
 def ffuse_profile_enable(on: bool):

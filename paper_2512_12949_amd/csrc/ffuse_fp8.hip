@@ -32,10 +32,12 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
 // Computed transposed like the other block GEMMs: the MFMA "A" operand is B, so that a lane has four neighbouring
 // columns of one row of Y.
 //
-// A step multiplies one stage, 16 rows after 16 rows: the fragments of the tile's columns stay in registers, those of the next
-// 16 rows are read under the MFMAs of the present ones, and each MFMA is followed by the multiply-adds of the one four before
-// it.  The workgroup meets before the last 16 rows, whose fragments are in registers by then: the next stage has landed, the
-// present one is free for the loads of the stage NS further on, and the last MFMAs cover the reads of the next step's first fragments.
+// A step multiplies one stage, 16 rows after 16 rows: the fragments of the wave's columns stay in registers, those of a row
+// block are read two blocks ahead, and beside each MFMA run the multiply-adds of the one four before it.  The workgroup meets before
+// the last two row blocks, whose fragments are in registers by then: the next stage has landed, and the present one is free
+// for the loads of the stage NS further on.  Those two go through the columns together, so that a column's fragment is free for
+// the next step's after two products and its reads spread over eight.  (One row block behind the barrier, read one block
+// ahead: 4096 x 4096 x 16384 in 247 us instead of 237.)
 template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct Fp8Gemm {
     static constexpr int NW = WM * WN, WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wave issues the same number of loads");
@@ -128,19 +130,15 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
         return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
     }
     struct Frags {
-        i32x8 a[HT], b[2];
-        f32x4 sw[BLOCK == 1 ? HT : 1];
-        float sw0, s[2];
+        i32x8 a[HT], b[4];   // the columns' fragments; those of the last row blocks read
+        float s[4];          // and their rows' scales
     };
-    // what a step starts with: the columns' fragments and scales, and the first 16 rows'
     static __device__ __forceinline__ void read_a(const char* stage, const Ctx& c, Frags& f, int ht) {
         f.a[ht] = frag(stage + c.rdw + 2048 * ht, stage + (c.rdw ^ 64u) + 2048 * ht);
-        if (BLOCK == 1) f.sw[BLOCK == 1 ? ht : 0] = *reinterpret_cast<const f32x4*>(stage + c.sw + 64 * ht);
-        else if (ht == 0) f.sw0 = *reinterpret_cast<const float*>(stage + c.sw);
     }
-    static __device__ __forceinline__ void read_b(const char* stage, const Ctx& c, Frags& f, int mt) {
-        f.b[mt & 1] = frag(stage + c.rdx + 2048 * mt, stage + (c.rdx ^ 64u) + 2048 * mt);
-        f.s[mt & 1] = *reinterpret_cast<const float*>(stage + c.sx + 64 * mt);
+    static __device__ __forceinline__ void read_b(const char* stage, const Ctx& c, Frags& f, int mt, int place) {
+        f.b[place] = frag(stage + c.rdx + 2048 * mt, stage + (c.rdx ^ 64u) + 2048 * mt);
+        f.s[place] = *reinterpret_cast<const float*>(stage + c.sx + 64 * mt);
     }
     // filled: the first stages were issued before the epilogue of the item before, whose stores are younger
     static __device__ __forceinline__ void run(char* smem, const Ctx& c, f32x4 (&acc)[HT][MT], int wave, bool filled) {
@@ -156,53 +154,62 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
         __syncthreads();
         Frags f;
         f32x4 part[LAG];
-        read_b(smem, c, f, 0);
+        read_b(smem, c, f, 0, 0);
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) read_a(smem, c, f, ht);
+        read_b(smem, c, f, 1, 1);
+        constexpr int FIRST = MT % 4 ? 2 : 0;   // where the next step's first row blocks are read to
         int slot = 0;
         for (int s = 0; s < KT; ++s) {
             const char* cur = smem + slot * STAGE;
             const uint32_t ld = lds + (uint32_t)(slot * STAGE);
             slot = slot == NS - 1 ? 0 : slot + 1;
             const char* nxt = smem + slot * STAGE;
-            f32x4 sw[HT];     // this step's column scales: the last multiply-adds run after the next ones are read
+            // the columns' scales, first used LAG products on
+            f32x4 sw[BLOCK == 1 ? HT : 1];
+            float sw0 = 1.0f, row[4];
+            if (BLOCK == 1) {
 #pragma unroll
-            for (int ht = 0; ht < HT; ++ht) sw[ht] = BLOCK == 1 ? f.sw[BLOCK == 1 ? ht : 0] : f32x4{f.sw0, f.sw0, f.sw0, f.sw0};
-            float row[2];
-            // MFMA i: rows i / HT, columns i % HT; the multiply-adds of part j beside it
+                for (int ht = 0; ht < (BLOCK == 1 ? HT : 1); ++ht) sw[ht] = *reinterpret_cast<const f32x4*>(cur + c.sw + 64 * ht);
+            } else {
+                sw0 = *reinterpret_cast<const float*>(cur + c.sw);
+            }
+            // MFMA i: row block mt, columns ht; the last two row blocks go through the columns together
+            constexpr int JOINT = NM - 2 * HT;
+            auto mt_of = [](int i) { return i < JOINT ? i / HT : MT - 2 + ((i - JOINT) & 1); };
+            auto ht_of = [](int i) { return i < JOINT ? i % HT : (i - JOINT) / 2; };
             auto add = [&](int j) {
-                const int mt = j / HT, ht = j % HT;
-                if (BLOCK == 1) {
+                const int mt = mt_of(j), ht = ht_of(j);
+                if (ht == 0) row[mt & 3] = BLOCK == 1 ? f.s[mt & 3] : f.s[mt & 3] * sw0;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[ht][mt][r] = __builtin_fmaf(part[j % LAG][r], sw[ht][r] * row[mt & 1], acc[ht][mt][r]);
-                } else {
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[ht][mt][r] = __builtin_fmaf(part[j % LAG][r], row[mt & 1], acc[ht][mt][r]);
-                }
+                for (int r = 0; r < 4; ++r)
+                    acc[ht][mt][r] = __builtin_fmaf(part[j % LAG][r], BLOCK == 1 ? sw[BLOCK == 1 ? ht : 0][r] * row[mt & 3] : row[mt & 3], acc[ht][mt][r]);
             };
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
-                const int mt = i / HT, ht = i % HT;
+                const int mt = mt_of(i), ht = ht_of(i);
                 if (i >= LAG) add(i - LAG);
-                if (ht == 0) {
-                    row[mt & 1] = BLOCK == 1 ? f.s[mt & 1] : f.s[mt & 1] * sw[0][0];
-                    if (mt + 1 < MT) read_b(cur, c, f, mt + 1);
-                    if (mt == MT - 1) {
-                        lds_loads_in_flight_at_most<(NS - 2) * NLOAD>();
-                        __syncthreads();
-                    }
+                if (ht == 0 && mt + 2 < MT) read_b(cur, c, f, mt + 2, (mt + 2) & 3);
+                if (i == JOINT) {
+                    lds_loads_in_flight_at_most<(NS - 2) * NLOAD>();
+                    __syncthreads();
                 }
-                part[i % LAG] = mma_e4m3(f.a[ht], f.b[mt & 1], zero);
-                if (mt == MT - 1) {
-                    if (ht == 0) read_b(nxt, c, f, 0);
-                    read_a(nxt, c, f, ht);
+                part[i % LAG] = mma_e4m3(f.a[ht], f.b[mt & 3], zero);
+                if (i >= JOINT) {
+                    const int p = i - JOINT;
+                    if (p & 1) read_a(nxt, c, f, ht);
+                    else if (p < 4) read_b(nxt, c, f, p / 2, FIRST + p / 2);
 #pragma unroll
-                    for (int e = (ht * NLOAD) / HT; e < ((ht + 1) * NLOAD) / HT; ++e) issue_one(c, ld, s + NS, e, wave);
+                    for (int e = p * NLOAD / (2 * HT); e < (p + 1) * NLOAD / (2 * HT); ++e) issue_one(c, ld, s + NS, e, wave);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int j = NM - LAG; j < NM; ++j) add(j);
+            if (FIRST) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) { f.b[j] = f.b[FIRST + j]; f.s[j] = f.s[FIRST + j]; }
+            }
         }
         __syncthreads();   // the stages are the next item's
     }
@@ -273,6 +280,99 @@ __global__ __launch_bounds__(64 * WM * WN) void fp8_product_kernel(Fp8Args a) {
         it = next;
     }
     lds_loads_in_flight_at_most<0>();   // (the last steps' loads write to LDS, if only zeros: not after the workgroup is gone)
+}
+
+// Few rows: the weights' way from memory is all that counts.  A workgroup has 16 columns and 16 MT rows, its eight waves every
+// eighth block of 128 k each, and a wave two blocks in flight, straight from memory to the registers of the matrix
+// instruction (16 rows of B x 128 bytes, whole cache lines, are its operand as they lie); the waves' sums meet in LDS.
+template <typename T, int MT, int BLOCK> __global__ __launch_bounds__(512) void fp8_stream_kernel(Fp8Args a) {
+    constexpr int NW = 8, DEPTH = 2;
+    __shared__ __attribute__((aligned(16))) f32x4 sums[NW][MT][64];
+    extern __shared__ __attribute__((aligned(16))) char table[];
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const uint32_t x = lane & 15, g = lane >> 4;
+    GroupItem it;
+    const int ncol = (a.N + 15) / 16, KB = (a.K + 127) / 128, NB = (a.N + BLOCK - 1) / BLOCK;
+    if (a.offsets) {
+        Groups groups;
+        scan_groups(groups, table, reinterpret_cast<char*>(sums), a.offsets, a.E, a.R, 16 * MT, tid);
+        if (!group_item(groups, 16 * MT, ncol, blockIdx.x & 7, blockIdx.x >> 3, it)) return;
+    } else {
+        it.e = 0;
+        it.row0 = (int64_t)(blockIdx.x / (uint32_t)ncol) * (16 * MT);
+        if (it.row0 >= a.R) return;
+        it.rows = a.R - (int)it.row0;
+        it.col = (int)(blockIdx.x % (uint32_t)ncol);
+    }
+    const int n0 = 16 * it.col, rows = min(it.rows, 16 * MT), cols = min(a.N - n0, 16);
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(a.A) + it.row0 * a.K, (uint32_t)rows * (uint32_t)a.K);
+    const __amdgpu_buffer_rsrc_t rw = make_rsrc(static_cast<const char*>(a.B) + ((int64_t)it.e * a.N + n0) * a.K, (uint32_t)cols * (uint32_t)a.K);
+    const float* sa = a.sa + it.row0;
+    const float* sb = a.sb + (int64_t)it.e * KB * NB + n0 / BLOCK;
+    uint32_t xo[MT], so[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+        const uint32_t row = (uint32_t)min(16 * mt + (int)x, rows - 1);
+        xo[mt] = row * (uint32_t)a.K + 16u * g;
+        so[mt] = 4u * row;
+    }
+    const uint32_t wo = (uint32_t)min((int)x, cols - 1) * (uint32_t)a.K + 16u * g;
+    const uint32_t bo = BLOCK == 1 ? 16u * min(g, (uint32_t)(cols - 1) / 4u) : 0u;   // (columns come in eights)
+    struct Slot {
+        u32x4 w[2], x[MT][2];
+        f32x4 sw;
+        float sx[MT];
+    } t[DEPTH];
+    auto load = [&](Slot& d, int kb) {
+        const uint32_t k = 128u * (uint32_t)kb;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool ok = 128 * kb + 64 * h + 16 * (int)g < a.K;
+            d.w[h] = buf_load16(rw, ok ? wo + k + 64u * h : kOob);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) d.x[mt][h] = buf_load16(rx, ok ? xo[mt] + k + 64u * h : kOob);
+        }
+        const bool ok = kb < KB;
+        const __amdgpu_buffer_rsrc_t ra = make_rsrc(sa + (int64_t)kb * a.R, ok ? 4u * (uint32_t)rows : 0u);
+        const __amdgpu_buffer_rsrc_t rb = make_rsrc(sb + (int64_t)kb * NB, ok ? 4u * (uint32_t)(BLOCK == 1 ? cols : 1) : 0u);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) d.sx[mt] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(ra, so[mt], 0, 0));
+        if (BLOCK == 1) d.sw = __builtin_bit_cast(f32x4, buf_load16(rb, bo));
+        else d.sw[0] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rb, 0, 0, 0));
+    };
+    f32x4 acc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const Slot& d) {
+        const i32x8 w = __builtin_shufflevector(__builtin_bit_cast(i32x4, d.w[0]), __builtin_bit_cast(i32x4, d.w[1]), 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            const i32x8 r = __builtin_shufflevector(__builtin_bit_cast(i32x4, d.x[mt][0]), __builtin_bit_cast(i32x4, d.x[mt][1]), 0, 1, 2, 3, 4, 5, 6, 7);
+            const f32x4 part = mma_e4m3(w, r, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[mt][e] = __builtin_fmaf(part[e], d.sx[mt] * d.sw[BLOCK == 1 ? e : 0], acc[mt][e]);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) load(t[d], wave + NW * d);
+    for (int kb = wave; kb < KB; kb += NW * DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            multiply(t[d]);
+            __builtin_amdgcn_sched_barrier(0);
+            load(t[d], kb + NW * (d + DEPTH));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) sums[wave][mt][lane] = acc[mt];
+    __syncthreads();
+    if (wave >= MT) return;
+    f32x4 y = sums[0][wave][lane];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) y += sums[w][wave][lane];
+    const int m = 16 * wave + (int)x, n = 4 * (int)g;
+    if (m < rows && n < cols)
+        *reinterpret_cast<uint2*>(static_cast<char*>(a.Y) + ((it.row0 + m) * a.N + n0 + n) * 2) = uint2{pack2<T>(y[0], y[1]), pack2<T>(y[2], y[3])};
 }
 
 // ---- quantising -------------------------------------------------------------------------------------------------
@@ -413,9 +513,23 @@ template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t 
     return hipGetLastError();
 }
 // Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
-static constexpr Tile kFp8[] = {{256, 256, 1, 1.70f, 2.0f}, {128, 256, 1, 0.98f, 2.0f}, {128, 128, 1, 0.58f, 2.0f},
-                                {64, 128, 1, 0.37f, 1.5f}, {32, 128, 1, 0.31f, 1.5f}, {64, 64, 2, 0.43f, 1.5f}};
+static constexpr Tile kFp8[] = {{256, 256, 1, 1.75f, 2.0f}, {128, 256, 1, 0.98f, 2.0f}, {128, 128, 1, 0.58f, 2.0f},
+                                {64, 128, 1, 0.37f, 1.5f}, {32, 128, 1, 0.32f, 1.5f}, {64, 64, 2, 0.42f, 1.5f}};
+template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStream_t st) {
+    const int64_t items = most_row_blocks(a.R, a.E, 16 * MT) * ((a.N + 15) / 16);
+    const dim3 grid((unsigned)((items + 7) / 8 * 8)), threads(512);
+    const int table = a.offsets ? group_table_bytes(a.E) : 0;
+    if (a.block == 1) hipLaunchKernelGGL((fp8_stream_kernel<T, MT, 1>), grid, threads, table, st, a);
+    else hipLaunchKernelGGL((fp8_stream_kernel<T, MT, 128>), grid, threads, table, st, a);
+    return hipGetLastError();
+}
 template <typename T> static hipError_t product_any(const Fp8Args& a, int cus, hipStream_t st) {
+    // Few rows: the streaming kernel, while its items are few enough to be under way together.  us, tiles -> this: one row of 4096 x
+    // 11008 14.6 -> 13.8 (weights not in any cache), 11008 x 4096 29 -> 13, 2048 x 2048 8.2 -> 3.6, 8192 x 28672 46 -> 45; 32 rows of
+    // 4096 x 4096 13.0 -> 8.6, of 4096 x 11008 13.4 -> 14.1.  512 rows in 64 groups 33 -> 84: each of many short items finds its group anew.
+    const int64_t groups = a.R < a.E ? a.R : a.E, columns = (a.N + 15) / 16;
+    if (a.R <= 16 * groups && most_row_blocks(a.R, a.E, 16) * columns <= (int64_t)8 * cus && (a.E == 1 || a.R <= 4 * groups)) return stream<T, 1>(a, st);
+    if (a.E == 1 && a.R <= 32 && columns <= (int64_t)2 * cus) return stream<T, 2>(a, st);
     switch (pick_tile(kFp8, a.R, a.E, a.N, a.K, cus)) {
         case 0: return product<T, 256, 256, 2, 4, 2>(a, cus, 1, st);
         case 1: return product<T, 128, 256, 2, 4, 2>(a, cus, 1, st);
