@@ -38,8 +38,8 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
 // for the loads of the stage NS further on.  Those two go through the columns together, so that a column's fragment is free for
 // the next step's after two products and its reads spread over eight.  (One row block behind the barrier, read one block
 // ahead: 4096 x 4096 x 16384 in 247 us instead of 237.)
-template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct Fp8Gemm {
-    static constexpr int NW = WM * WN, WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;
+template <typename T, int BM_, int BN_, int WM, int WN, int NS, int BLOCK_> struct Fp8Gemm {
+    static constexpr int BM = BM_, BN = BN_, BLOCK = BLOCK_, NW = WM * WN, WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wave issues the same number of loads");
     static_assert(BLOCK == 1 || BLOCK == 128, "scales of B");
     static_assert(128 % WNR == 0, "a wave's columns share a block of 128");
@@ -246,40 +246,49 @@ template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK> struct 
     }
 };
 
-template <typename T, int BM, int BN, int WM, int WN, int NS, int BLOCK>
-__global__ __launch_bounds__(64 * WM * WN) void fp8_product_kernel(Fp8Args a) {
-    typedef Fp8Gemm<T, BM, BN, WM, WN, NS, BLOCK> G;
-    static_assert(G::LDS_BYTES <= kLdsBesideGroups, "LDS");
-    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
-    extern __shared__ __attribute__((aligned(16))) char table[];
-    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    Groups groups;
-    scan_groups(groups, table, smem, a.offsets, a.E, a.R, BM, tid);
+template <class G, class Walk> __device__ __forceinline__ void fp8_rows(const Fp8Args& a, char* smem, Walk&& walk, int tid, int wave) {
     f32x4 acc[G::HT][G::MT];
     typename G::Ctx c;
     G::init_lds(c, tid);
-    const int ncol = (a.N + BN - 1) / BN, KB = (a.K + 127) / 128, NB = (a.N + BLOCK - 1) / BLOCK;
+    const int KB = (a.K + 127) / 128, NB = (a.N + G::BLOCK - 1) / G::BLOCK;
     GroupItem it, next;
-    int idx = blockIdx.x >> 3;
-    bool have = group_item(groups, BM, ncol, xcd, idx, it), filled = false;
+    bool have = walk.next(it), filled = false;
     auto aim = [&](const GroupItem& i) {
-        const int n0 = i.col * BN;
         G::aim(c, static_cast<const char*>(a.A) + i.row0 * a.K, a.sa + i.row0, a.R, i.rows,
-               static_cast<const char*>(a.B) + ((int64_t)i.e * a.N + n0) * a.K, a.sb + (int64_t)i.e * KB * NB + n0 / BLOCK, NB, a.N - n0, a.K, tid);
+               static_cast<const char*>(a.B) + ((int64_t)i.e * a.N + i.col) * a.K, a.sb + (int64_t)i.e * KB * NB + i.col / G::BLOCK, NB, a.N - i.col, a.K, tid);
         G::fill(smem, c, wave);
     };
     if (have) aim(it);
     while (have) {
         G::run(smem, c, acc, wave, filled);
-        idx += step;
-        have = group_item(groups, BM, ncol, xcd, idx, next);
+        have = walk.next(next);
         if (have) aim(next);
         filled = true;
-        const int n0 = it.col * BN;
-        G::store(smem, acc, static_cast<char*>(a.Y) + (it.row0 * a.N + n0) * 2, (uint32_t)a.N, it.rows, a.N - n0, wave);
+        G::store(smem, acc, static_cast<char*>(a.Y) + (it.row0 * a.N + it.col) * 2, (uint32_t)a.N, it.rows, a.N - it.col, wave);
         it = next;
     }
-    lds_loads_in_flight_at_most<0>();   // (the last steps' loads write to LDS, if only zeros: not after the workgroup is gone)
+    // (the last steps' loads write to LDS, if only zeros: not after it is somebody else's)
+    lds_loads_in_flight_at_most<0>();
+}
+// G: the tile of an item; S: of its parts (whole_items), `cost` of it each, or G itself
+template <class G, class S> __global__ __launch_bounds__(64 * G::NW) void fp8_product_kernel(Fp8Args a, float cost) {
+    constexpr int PARTS = (G::BM / S::BM) * (G::BN / S::BN), LDS = G::LDS_BYTES > S::LDS_BYTES ? G::LDS_BYTES : S::LDS_BYTES;
+    static_assert(LDS <= kLdsBesideGroups, "LDS");
+    static_assert(G::NW == S::NW, "one workgroup does both");
+    __shared__ __attribute__((aligned(16))) char smem[LDS];
+    extern __shared__ __attribute__((aligned(16))) char table[];
+    const int tid = threadIdx.x, xcd = blockIdx.x & 7, loc = blockIdx.x >> 3, step = gridDim.x >> 3, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    Groups groups;
+    scan_groups(groups, table, smem, a.offsets, a.E, a.R, G::BM, tid);
+    const int ncol = (a.N + G::BN - 1) / G::BN;
+    const int items = group_items(groups, ncol, xcd), whole = PARTS > 1 ? whole_items<PARTS>(items, step, cost) : items;
+    fp8_rows<G>(a, smem, ItemWalk<G::BM, G::BN, 1>{groups, G::BM, G::BN, ncol, a.N, xcd, 0, whole, step, loc}, tid, wave);
+    if constexpr (PARTS > 1) {
+        if (whole < items) {
+            __syncthreads();
+            fp8_rows<S>(a, smem, ItemWalk<S::BM, S::BN, PARTS>{groups, G::BM, G::BN, ncol, a.N, xcd, whole, items - whole, step, loc}, tid, wave);
+        }
+    }
 }
 
 // Few rows: the weights' way from memory is all that counts.  A workgroup has 16 columns and 16 MT rows, its eight waves every
@@ -296,15 +305,17 @@ template <typename T, int MT, int BLOCK> __global__ __launch_bounds__(512) void 
     if (a.offsets) {
         Groups groups;
         scan_groups(groups, table, reinterpret_cast<char*>(sums), a.offsets, a.E, a.R, 16 * MT, tid);
-        if (!group_item(groups, 16 * MT, ncol, blockIdx.x & 7, blockIdx.x >> 3, it)) return;
+        const int xcd = blockIdx.x & 7, idx = blockIdx.x >> 3;
+        if (idx >= group_items(groups, ncol, xcd)) return;
+        it = group_item(groups, 16 * MT, 16, ncol, xcd, idx);
     } else {
         it.e = 0;
         it.row0 = (int64_t)(blockIdx.x / (uint32_t)ncol) * (16 * MT);
         if (it.row0 >= a.R) return;
         it.rows = a.R - (int)it.row0;
-        it.col = (int)(blockIdx.x % (uint32_t)ncol);
+        it.col = 16 * (int)(blockIdx.x % (uint32_t)ncol);
     }
-    const int n0 = 16 * it.col, rows = min(it.rows, 16 * MT), cols = min(a.N - n0, 16);
+    const int n0 = it.col, rows = min(it.rows, 16 * MT), cols = min(a.N - n0, 16);
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(static_cast<const char*>(a.A) + it.row0 * a.K, (uint32_t)rows * (uint32_t)a.K);
     const __amdgpu_buffer_rsrc_t rw = make_rsrc(static_cast<const char*>(a.B) + ((int64_t)it.e * a.N + n0) * a.K, (uint32_t)cols * (uint32_t)a.K);
     const float* sa = a.sa + it.row0;
@@ -505,11 +516,9 @@ template <typename T, int BLOCK> __global__ __launch_bounds__(256) void quantize
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------
-template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t product(const Fp8Args& a, int cus, int per_cu, hipStream_t st) {
-    const int64_t items = most_row_blocks(a.R, a.E, BM) * ((a.N + BN - 1) / BN);
-    const dim3 grid(persistent_grid(items, cus, per_cu)), threads(64 * WM * WN);
-    if (a.block == 1) hipLaunchKernelGGL((fp8_product_kernel<T, BM, BN, WM, WN, NS, 1>), grid, threads, group_table_bytes(a.E), st, a);
-    else hipLaunchKernelGGL((fp8_product_kernel<T, BM, BN, WM, WN, NS, 128>), grid, threads, group_table_bytes(a.E), st, a);
+template <class G, class S> static hipError_t product(const Fp8Args& a, int cus, int per_cu, float cost, hipStream_t st) {
+    const int64_t items = most_row_blocks(a.R, a.E, G::BM) * ((a.N + G::BN - 1) / G::BN);
+    hipLaunchKernelGGL((fp8_product_kernel<G, S>), dim3(persistent_grid(items, cus, per_cu)), dim3(64 * G::NW), group_table_bytes(a.E), st, a, cost);
     return hipGetLastError();
 }
 // Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
@@ -523,6 +532,22 @@ template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStre
     else hipLaunchKernelGGL((fp8_stream_kernel<T, MT, 128>), grid, threads, table, st, a);
     return hipGetLastError();
 }
+template <typename T, int BLOCK> static hipError_t tiles(const Fp8Args& a, int cus, hipStream_t st) {
+    typedef Fp8Gemm<T, 256, 256, 2, 4, 2, BLOCK> G256;
+    typedef Fp8Gemm<T, 128, 128, 4, 2, 4, BLOCK> G128;
+    typedef Fp8Gemm<T, 128, 256, 2, 4, 2, BLOCK> W128;
+    typedef Fp8Gemm<T, 64, 128, 2, 4, 5, BLOCK> G64;
+    typedef Fp8Gemm<T, 32, 128, 1, 4, 6, BLOCK> G32;
+    typedef Fp8Gemm<T, 64, 64, 2, 2, 4, BLOCK> S64;
+    switch (pick_tile(kFp8, a.R, a.E, a.N, a.K, cus)) {
+        case 0: return product<G256, G128>(a, cus, 1, 0.34f, st);
+        case 1: return product<W128, G64>(a, cus, 1, 0.39f, st);
+        case 2: return product<G128, G64>(a, cus, 1, 0.64f, st);
+        case 3: return product<G64, G64>(a, cus, 1, 1.0f, st);
+        case 4: return product<G32, G32>(a, cus, 1, 1.0f, st);
+        default: return product<S64, S64>(a, cus, 2, 1.0f, st);
+    }
+}
 template <typename T> static hipError_t product_any(const Fp8Args& a, int cus, hipStream_t st) {
     // Few rows: the streaming kernel, while its items are few enough to be under way together.  us, tiles -> this: one row of 4096 x
     // 11008 14.6 -> 13.8 (weights not in any cache), 11008 x 4096 29 -> 13, 2048 x 2048 8.2 -> 3.6, 8192 x 28672 46 -> 45; 32 rows of
@@ -530,14 +555,7 @@ template <typename T> static hipError_t product_any(const Fp8Args& a, int cus, h
     const int64_t groups = a.R < a.E ? a.R : a.E, columns = (a.N + 15) / 16;
     if (a.R <= 16 * groups && most_row_blocks(a.R, a.E, 16) * columns <= (int64_t)8 * cus && (a.E == 1 || a.R <= 4 * groups)) return stream<T, 1>(a, st);
     if (a.E == 1 && a.R <= 32 && columns <= (int64_t)2 * cus) return stream<T, 2>(a, st);
-    switch (pick_tile(kFp8, a.R, a.E, a.N, a.K, cus)) {
-        case 0: return product<T, 256, 256, 2, 4, 2>(a, cus, 1, st);
-        case 1: return product<T, 128, 256, 2, 4, 2>(a, cus, 1, st);
-        case 2: return product<T, 128, 128, 4, 2, 4>(a, cus, 1, st);
-        case 3: return product<T, 64, 128, 2, 4, 5>(a, cus, 1, st);
-        case 4: return product<T, 32, 128, 1, 4, 6>(a, cus, 1, st);
-        default: return product<T, 64, 64, 2, 2, 4>(a, cus, 2, st);
-    }
+    return a.block == 1 ? tiles<T, 1>(a, cus, st) : tiles<T, 128>(a, cus, st);
 }
 hipError_t launch_fp8_product(int dtype, const Fp8Args& a, int cus, hipStream_t st) {
     return dtype == 0 ? product_any<__bf16>(a, cus, st) : product_any<_Float16>(a, cus, st);

@@ -162,8 +162,9 @@ template <typename T, int COLS, int MT> struct TileStore {
     }
 };
 
-template <typename T, bool ACOL, bool BCOL, bool GATED, int BM, int BN, int WM, int WN, int NS> struct PairGemm {
+template <typename T, bool ACOL, bool BCOL, bool GATED, int BM_, int BN_, int WM, int WN, int NS> struct PairGemm {
     typedef typename Mma<T>::vec8 vec8;
+    static constexpr int BM = BM_, BN = BN_;
     static constexpr int NW = WM * WN, G = GATED ? 2 : 1;
     static constexpr int WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;   // a wave's rows, columns and 16 x 16 tiles
     static_assert(WMR % 32 == 0 && WNR % 16 == 0, "16 x 16 tiles, an even number of row blocks");

@@ -16,43 +16,57 @@ namespace ffuse {
 // ---- forward, and the gradient of the input -------------------------------------------------------------------------
 // The rows of each group times its matrix, or its transpose: persistent workgroups; an item's first loads go out
 // before the epilogue of the one before.  BCOL: Y = act(A W) (.* A W3), W [E][K][N]; otherwise Y = A W^T, W [E][N][K].
-template <typename T, bool BCOL, bool GATED, int BM, int BN, int WM, int WN, int NS>
-__global__ __launch_bounds__(64 * WM * WN) void grouped_rows_kernel(GroupedArgs a) {
-    typedef PairGemm<T, false, BCOL, GATED, BM, BN, WM, WN, NS> G;
-    static_assert(G::LDS_BYTES <= kLdsBesideGroups, "LDS");
-    __shared__ __attribute__((aligned(16))) char smem[G::LDS_BYTES];
-    extern __shared__ __attribute__((aligned(16))) char table[];
-    const int tid = threadIdx.x, xcd = blockIdx.x & 7, step = gridDim.x >> 3, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    Groups groups;
-    scan_groups(groups, table, smem, a.offsets, a.E, a.R, BM, tid);
+template <typename T, bool BCOL, bool GATED, class G, class Walk>
+__device__ __forceinline__ void grouped_rows(const GroupedArgs& a, char* smem, Walk&& walk, int wave, int lane) {
     f32x4 acc[G::G][G::HT][G::MT];
     typename G::Ctx c;
     G::init(c, wave, lane);
-    const int K = c.K = BCOL ? a.K : a.N, N = BCOL ? a.N : a.K, ncol = (N + BN - 1) / BN;
+    const int K = c.K = BCOL ? a.K : a.N, N = BCOL ? a.N : a.K;
     GroupItem it, next;
-    int idx = blockIdx.x >> 3;
-    bool have = group_item(groups, BM, ncol, xcd, idx, it), filled = false;
+    bool have = walk.next(it), filled = false;
     auto aim = [&](const GroupItem& i) {
-        const int n0 = i.col * BN;
         c.a.aim(static_cast<const char*>(a.A) + i.row0 * K * 2, K, i.rows, K, wave, lane);
-        const int64_t w = ((int64_t)i.e * K * N + (BCOL ? n0 : (int64_t)n0 * K)) * 2;
-        c.b[0].aim(static_cast<const char*>(a.W) + w, BCOL ? N : K, N - n0, K, wave, lane);
-        if (GATED) c.b[G::G - 1].aim(static_cast<const char*>(a.W3) + w, BCOL ? N : K, N - n0, K, wave, lane);
+        const int64_t w = ((int64_t)i.e * K * N + (BCOL ? i.col : (int64_t)i.col * K)) * 2;
+        c.b[0].aim(static_cast<const char*>(a.W) + w, BCOL ? N : K, N - i.col, K, wave, lane);
+        if (GATED) c.b[G::G - 1].aim(static_cast<const char*>(a.W3) + w, BCOL ? N : K, N - i.col, K, wave, lane);
         G::fill(smem, c);
     };
     if (have) aim(it);
     while (have) {
         G::run(smem, c, acc, filled);
-        idx += step;
-        have = group_item(groups, BM, ncol, xcd, idx, next);
+        have = walk.next(next);
         if (have) aim(next);
         filled = true;
-        char* Y = static_cast<char*>(a.C) + (it.row0 * N + it.col * BN) * 2;
-        if (BCOL) G::store_rt(smem, a.act, acc, Y, (uint32_t)N, it.rows, N - it.col * BN, wave);
-        else G::template store<ACT_IDENTITY>(smem, acc, Y, (uint32_t)N, it.rows, N - it.col * BN, wave);
+        char* Y = static_cast<char*>(a.C) + (it.row0 * N + it.col) * 2;
+        if (BCOL) G::store_rt(smem, a.act, acc, Y, (uint32_t)N, it.rows, N - it.col, wave);
+        else G::template store<ACT_IDENTITY>(smem, acc, Y, (uint32_t)N, it.rows, N - it.col, wave);
         it = next;
     }
-    lds_loads_in_flight_at_most<0>();   // (the last steps' loads write to LDS, if only zeros: not after the workgroup is gone)
+    // (the last steps' loads write to LDS, if only zeros: not after it is somebody else's)
+    lds_loads_in_flight_at_most<0>();
+}
+
+// G: the tile of an item; S: of its parts (whole_items), `cost` of it each, or G itself
+template <typename T, bool BCOL, bool GATED, class G, class S>
+__global__ __launch_bounds__(64 * G::NW) void grouped_rows_kernel(GroupedArgs a, float cost) {
+    constexpr int PARTS = (G::BM / S::BM) * (G::BN / S::BN), LDS = G::LDS_BYTES > S::LDS_BYTES ? G::LDS_BYTES : S::LDS_BYTES;
+    static_assert(LDS <= kLdsBesideGroups, "LDS");
+    static_assert(G::NW == S::NW, "one workgroup does both");
+    __shared__ __attribute__((aligned(16))) char smem[LDS];
+    extern __shared__ __attribute__((aligned(16))) char table[];
+    const int tid = threadIdx.x, xcd = blockIdx.x & 7, loc = blockIdx.x >> 3, step = gridDim.x >> 3, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    Groups groups;
+    scan_groups(groups, table, smem, a.offsets, a.E, a.R, G::BM, tid);
+    const int N = BCOL ? a.N : a.K, ncol = (N + G::BN - 1) / G::BN;
+    const int items = group_items(groups, ncol, xcd), whole = PARTS > 1 ? whole_items<PARTS>(items, step, cost) : items;
+    grouped_rows<T, BCOL, GATED, G>(a, smem, ItemWalk<G::BM, G::BN, 1>{groups, G::BM, G::BN, ncol, N, xcd, 0, whole, step, loc}, wave, lane);
+    if constexpr (PARTS > 1) {
+        if (whole < items) {
+            __syncthreads();
+            grouped_rows<T, BCOL, GATED, S>(a, smem, ItemWalk<S::BM, S::BN, PARTS>{groups, G::BM, G::BN, ncol, N, xcd, whole, items - whole, step, loc}, wave, lane);
+        }
+    }
 }
 
 // ---- gradient of the weights ------------------------------------------------------------------------------------
@@ -92,29 +106,42 @@ static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f}, {128, 256, 1, 0.92
 static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f}, {128, 256, 1, 0.90f, 2.0f}, {64, 256, 1, 0.65f, 2.0f},
                                   {64, 128, 1, 0.38f, 2.0f}, {32, 128, 1, 0.28f, 2.0f}, {64, 64, 2, 0.45f, 2.0f}};
 
-template <typename T, bool BCOL, bool GATED, int BM, int BN, int WM, int WN, int NS> static hipError_t rows(const GroupedArgs& a, int cus, int per_cu, hipStream_t st) {
+template <typename T, bool BCOL, bool GATED, class G, class S> static hipError_t rows(const GroupedArgs& a, int cus, int per_cu, float cost, hipStream_t st) {
     const int N = BCOL ? a.N : a.K;
-    const int grid = persistent_grid(most_row_blocks(a.R, a.E, BM) * ((N + BN - 1) / BN), cus, per_cu);
-    hipLaunchKernelGGL((grouped_rows_kernel<T, BCOL, GATED, BM, BN, WM, WN, NS>), dim3(grid), dim3(64 * WM * WN), group_table_bytes(a.E), st, a);
+    const int grid = persistent_grid(most_row_blocks(a.R, a.E, G::BM) * ((N + G::BN - 1) / G::BN), cus, per_cu);
+    hipLaunchKernelGGL((grouped_rows_kernel<T, BCOL, GATED, G, S>), dim3(grid), dim3(64 * G::NW), group_table_bytes(a.E), st, a, cost);
     return hipGetLastError();
 }
 template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hipStream_t st) {
+    typedef PairGemm<T, false, true, true, 256, 128, 2, 4, 2> G256;
+    typedef PairGemm<T, false, true, true, 128, 64, 4, 2, 4> Q256;
+    typedef PairGemm<T, false, true, true, 128, 128, 2, 4, 3> G128;
+    typedef PairGemm<T, false, true, true, 64, 128, 2, 4, 3> G64;
+    typedef PairGemm<T, false, true, true, 32, 128, 1, 4, 3> G32;
+    typedef PairGemm<T, false, true, true, 64, 64, 2, 2, 3> S64;
     switch (pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus)) {
-        case 0: return rows<T, true, true, 256, 128, 2, 4, 2>(a, cus, 1, st);
-        case 1: return rows<T, true, true, 128, 128, 2, 4, 3>(a, cus, 1, st);
-        case 2: return rows<T, true, true, 64, 128, 2, 4, 3>(a, cus, 1, st);
-        case 3: return rows<T, true, true, 32, 128, 1, 4, 3>(a, cus, 1, st);
-        default: return rows<T, true, true, 64, 64, 2, 2, 3>(a, cus, 2, st);
+        case 0: return rows<T, true, true, G256, Q256>(a, cus, 1, 0.36f, st);
+        case 1: return rows<T, true, true, G128, G64>(a, cus, 1, 0.76f, st);
+        case 2: return rows<T, true, true, G64, G64>(a, cus, 1, 1.0f, st);
+        case 3: return rows<T, true, true, G32, G32>(a, cus, 1, 1.0f, st);
+        default: return rows<T, true, true, S64, S64>(a, cus, 2, 1.0f, st);
     }
 }
 template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, int cus, hipStream_t st) {
+    typedef PairGemm<T, false, BCOL, false, 256, 256, 2, 4, 2> G256;
+    typedef PairGemm<T, false, BCOL, false, 128, 128, 2, 4, 4> Q256;
+    typedef PairGemm<T, false, BCOL, false, 128, 256, 2, 4, 3> G128;
+    typedef PairGemm<T, false, BCOL, false, 64, 256, 2, 4, 3> W64;
+    typedef PairGemm<T, false, BCOL, false, 64, 128, 2, 4, 4> G64;
+    typedef PairGemm<T, false, BCOL, false, 32, 128, 1, 4, 4> G32;
+    typedef PairGemm<T, false, BCOL, false, 64, 64, 2, 2, 4> S64;
     switch (BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus)) {
-        case 0: return rows<T, BCOL, false, 256, 256, 2, 4, 2>(a, cus, 1, st);
-        case 1: return rows<T, BCOL, false, 128, 256, 2, 4, 3>(a, cus, 1, st);
-        case 2: return rows<T, BCOL, false, 64, 256, 2, 4, 3>(a, cus, 1, st);
-        case 3: return rows<T, BCOL, false, 64, 128, 2, 4, 4>(a, cus, 1, st);
-        case 4: return rows<T, BCOL, false, 32, 128, 1, 4, 4>(a, cus, 1, st);
-        default: return rows<T, BCOL, false, 64, 64, 2, 2, 4>(a, cus, 2, st);
+        case 0: return rows<T, BCOL, false, G256, Q256>(a, cus, 1, 0.38f, st);
+        case 1: return rows<T, BCOL, false, G128, G64>(a, cus, 1, 0.46f, st);
+        case 2: return rows<T, BCOL, false, W64, G64>(a, cus, 1, 0.64f, st);
+        case 3: return rows<T, BCOL, false, G64, G64>(a, cus, 1, 1.0f, st);
+        case 4: return rows<T, BCOL, false, G32, G32>(a, cus, 1, 1.0f, st);
+        default: return rows<T, BCOL, false, S64, S64>(a, cus, 2, 1.0f, st);
     }
 }
 hipError_t launch_grouped_forward(int dtype, const GroupedArgs& a, int cus, hipStream_t st) {

@@ -72,17 +72,19 @@ struct GroupItem {
     int e;           // group
     int64_t row0;    // first row of the block
     int rows;        // rows of the group from there on (more than the block holds, or fewer)
-    int col;         // column block
+    int col;         // first column
 };
 
-// Item `idx` of XCD `xcd`: the items of an XCD are consecutive, the row blocks of a group in bands of kGroupBand,
-// column block by column block, so that the 32 workgroups of an XCD work on a patch of a band and a few column
-// blocks and fetch each panel of either operand into its L2 once.  ncol: column blocks.
-__device__ __forceinline__ bool group_item(const Groups& g, int bm, int ncol, int xcd, int idx, GroupItem& it) {
+// Items of `bm` rows x `bn` columns, `ncol` column blocks.  Those of an XCD are consecutive, the row blocks of a group in bands
+// of kGroupBand, column block by column block, so that the 32 workgroups of an XCD work on a patch of a band and a few column
+// blocks and fetch each panel of either operand into its L2 once.
+__device__ __forceinline__ int group_items(const Groups& g, int ncol, int xcd) {   // of an XCD
+    const int total = __builtin_amdgcn_readfirstlane(g.tiles[g.E - 1]) * ncol, per = (total + 7) >> 3;
+    return min(per, max(total - xcd * per, 0));
+}
+__device__ __forceinline__ GroupItem group_item(const Groups& g, int bm, int bn, int ncol, int xcd, int idx) {   // idx < group_items
     const int total = __builtin_amdgcn_readfirstlane(g.tiles[g.E - 1]) * ncol;
-    const int per = (total + 7) >> 3;
-    const int v = xcd * per + idx;
-    if (idx >= per || v >= total) return false;
+    const int v = xcd * ((total + 7) >> 3) + idx;
     const int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
     int e = 0;       // groups that end at or before the item
     for (int base = 0; base < g.E; base += 64) {
@@ -97,11 +99,37 @@ __device__ __forceinline__ bool group_item(const Groups& g, int bm, int ncol, in
     const int h = min(kGroupBand, nt - band * kGroupBand);
     const int c = in / h, r = band * kGroupBand + in - c * h;
     const int first = __builtin_amdgcn_readfirstlane(g.start[e]), last = __builtin_amdgcn_readfirstlane(e + 1 < g.E ? g.start[e + 1] : g.end);
-    it.e = e;
-    it.row0 = (int64_t)first + (int64_t)r * bm;
-    it.rows = last - first - r * bm;
-    it.col = c;
-    return true;
+    return {e, (int64_t)first + (int64_t)r * bm, last - first - r * bm, c * bn};
+}
+
+// One workgroup's share of an XCD's items: `count` of them, numbers loc, loc + step, ...; or, PARTS > 1, of the parts (PM rows x PN
+// columns) of the `count` items from `first` on.
+template <int PM, int PN, int PARTS> struct ItemWalk {
+    const Groups& g;
+    int bm, bn, ncol, cols, xcd, first, count, step, at;
+    __device__ __forceinline__ bool next(GroupItem& it) {
+        for (; at < count * PARTS; at += step) {
+            it = group_item(g, bm, bn, ncol, xcd, first + at / PARTS);
+            if (PARTS > 1) {
+                const int part = at % PARTS, down = bm / PM;
+                it.row0 += part % down * PM;
+                it.rows -= part % down * PM;
+                it.col += part / down * PN;
+                if (it.rows <= 0 || it.col >= cols) continue;
+            }
+            at += step;
+            return true;
+        }
+        return false;
+    }
+};
+
+// The items of an XCD that its workgroups cannot all have one of: they are done in parts, where that is sooner (a part takes
+// `cost` of an item's time).  Returns the items that are left whole.
+template <int PARTS> __device__ __forceinline__ int whole_items(int items, int step, float cost) {
+    const int left = items % step;
+    if (items < step || left == 0) return items;
+    return (float)((left * PARTS + step - 1) / step) * cost < 0.95f ? items - left : items;
 }
 
 // ---- host side of the launches
