@@ -48,11 +48,10 @@ template <typename T, int BM_, int BN_, int WM, int WN, int NS, int BLOCK_> stru
     static constexpr int SI = (SA + SB + NW - 1) / NW;                    // ... per wave (some are issued twice)
     static constexpr int NLOAD = XI + BI + SI;
     static constexpr int XB = BM * 128, SOFF = XB + BN * 128, STAGE = SOFF + (SA + SB) * 256;
-    static constexpr int ROW = WNR * 2, SLOTS = ROW / 8;                  // epilogue: bytes and 8-byte slots of a staged row
-    static constexpr int EPI = NS * STAGE, LDS_BYTES = EPI + NW * 16 * ROW;
-    static_assert(ROW == 64 || ROW == 128, "the epilogue's swizzle");
-    static constexpr int LPR = ROW / 16, RPI = 64 / LPR;                  // lanes a row and rows an instruction on the way out
-    static constexpr int STORES = MT * (16 / RPI);
+    // (a wave's columns leave 32 at a time where the ring leaves no room for 64)
+    static constexpr int ECOL = WNR == 64 && NS * STAGE + NW * 2048 > 152 * 1024 ? 32 : WNR;
+    typedef TileStore<T, ECOL, MT> Store;
+    static constexpr int EPI = NS * STAGE, LDS_BYTES = EPI + NW * Store::LDS_BYTES, STORES = WNR / ECOL * MT * Store::STORES;
     static_assert(NS >= 2 && (NS - 1) * NLOAD + STORES <= 63, "the vmcnt field holds 6 bits");
     static_assert(MT % 2 == 0, "the last rows' fragments and the next step's first lie in different registers");
     static constexpr int NM = MT * HT, LAG = HT < 4 ? HT : 4;             // MFMAs a step; parts in flight
@@ -213,38 +212,18 @@ template <typename T, int BM_, int BN_, int WM, int WN, int NS, int BLOCK_> stru
         }
         __syncthreads();   // the stages are the next item's
     }
-    // Y: the tile's first row and column; through LDS of its own, 16 rows at a time, so that a row's part of the tile is stored in
-    // whole lines.  Every wave issues STORES stores, those past the tile's rows and columns out of range.
+    // Y: the tile's first row and column
     static __device__ __forceinline__ void store(char* smem, const f32x4 (&acc)[HT][MT], char* Y, uint32_t ldy, int have_m, int have_n, int wave) {
-        int lane = (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-        asm volatile("" : "+v"(lane));   // (otherwise the addresses below are computed before the main loop and kept through it)
-        const int wm = wave % WM, wn = wave / WM;
-        const uint32_t x = lane & 15, g = lane >> 4;
-        char* mine = smem + EPI + wave * 16 * ROW;
-        const uint32_t rin = lane / LPR, ch = lane % LPR;
-        const int col = wn * WNR + 8 * (int)ch;
-        const __amdgpu_buffer_rsrc_t ry = make_rsrc(Y, (uint32_t)min(have_m, BM) * 2u * ldy);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t key = (x >> (ROW == 128 ? 1 : 2)) & (SLOTS - 1);
-#pragma unroll
-            for (int ht = 0; ht < HT; ++ht) {
-                uint2 o;
-                o.x = pack2<T>(acc[ht][mt][0], acc[ht][mt][1]);
-                o.y = pack2<T>(acc[ht][mt][2], acc[ht][mt][3]);
-                *reinterpret_cast<uint2*>(mine + x * ROW + (((4 * ht + g) ^ key) << 3)) = o;
-            }
-#pragma unroll
-            for (int i = 0; i < 16 / RPI; ++i) {
-                const uint32_t row = i * RPI + rin, k = (row >> (ROW == 128 ? 1 : 2)) & (SLOTS - 1);
-                u32x4 v = *reinterpret_cast<const u32x4*>(mine + row * ROW + ((ch ^ (k >> 1)) << 4));
-                if (k & 1u) v = u32x4{v[2], v[3], v[0], v[1]};
-                const int m = wm * WMR + 16 * mt + (int)row;
-                __builtin_amdgcn_raw_buffer_store_b128(v, ry, m < have_m && col < have_n ? ((uint32_t)m * ldy + (uint32_t)col) * 2u : kOob, 0, 0);
-            }
-        }
+        for (int e = 0; e < WNR / ECOL; ++e)
+            Store::store(smem + EPI + wave * Store::LDS_BYTES, Y, ldy, wave % WM * WMR, wave / WM * WNR + e * ECOL, BM, have_m, have_n,
+                         [&](int h, int mt, int r) { return acc[e * (ECOL / 16) + h][mt][r]; });
     }
 };
+
+// LDS of the largest tile, which leaves room for the tables of kFp8Groups groups
+static constexpr int kFp8Lds = 160256, kFp8Groups = (160 * 1024 - kFp8Lds) / 8;
+static_assert(group_table_bytes(kFp8Groups) <= 160 * 1024 - kFp8Lds, "LDS");
 
 template <class G, class Walk> __device__ __forceinline__ void fp8_rows(const Fp8Args& a, char* smem, Walk&& walk, int tid, int wave) {
     f32x4 acc[G::HT][G::MT];
@@ -273,7 +252,7 @@ template <class G, class Walk> __device__ __forceinline__ void fp8_rows(const Fp
 // G: the tile of an item; S: of its parts (whole_items), `cost` of it each, or G itself
 template <class G, class S> __global__ __launch_bounds__(64 * G::NW) void fp8_product_kernel(Fp8Args a, float cost) {
     constexpr int PARTS = (G::BM / S::BM) * (G::BN / S::BN), LDS = G::LDS_BYTES > S::LDS_BYTES ? G::LDS_BYTES : S::LDS_BYTES;
-    static_assert(LDS <= kLdsBesideGroups, "LDS");
+    static_assert(LDS <= kFp8Lds, "LDS");
     static_assert(G::NW == S::NW, "one workgroup does both");
     __shared__ __attribute__((aligned(16))) char smem[LDS];
     extern __shared__ __attribute__((aligned(16))) char table[];
@@ -516,14 +495,14 @@ template <typename T, int BLOCK> __global__ __launch_bounds__(256) void quantize
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------
-template <class G, class S> static hipError_t product(const Fp8Args& a, int cus, int per_cu, float cost, hipStream_t st) {
+template <class G, class S> static hipError_t product(const Fp8Args& a, const Tile& t, int cus, hipStream_t st) {
     const int64_t items = most_row_blocks(a.R, a.E, G::BM) * ((a.N + G::BN - 1) / G::BN);
-    hipLaunchKernelGGL((fp8_product_kernel<G, S>), dim3(persistent_grid(items, cus, per_cu)), dim3(64 * G::NW), group_table_bytes(a.E), st, a, cost);
+    hipLaunchKernelGGL((fp8_product_kernel<G, S>), dim3(persistent_grid(items, cus, t.per_cu)), dim3(64 * G::NW), group_table_bytes(a.E), st, a, t.cost);
     return hipGetLastError();
 }
 // Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
-static constexpr Tile kFp8[] = {{256, 256, 1, 1.75f, 2.0f}, {128, 256, 1, 0.98f, 2.0f}, {128, 128, 1, 0.58f, 2.0f},
-                                {64, 128, 1, 0.37f, 1.5f}, {32, 128, 1, 0.32f, 1.5f}, {64, 64, 2, 0.42f, 1.5f}};
+static constexpr Tile kFp8[] = {{256, 256, 1, 1.68f, 2.0f, 4, 0.36f}, {128, 256, 1, 1.00f, 2.0f, 4, 0.39f}, {128, 128, 1, 0.58f, 2.0f, 2, 0.64f},
+                                {64, 128, 1, 0.37f, 1.5f, 1, 1.0f},   {32, 128, 1, 0.32f, 1.5f, 1, 1.0f},   {64, 64, 2, 0.42f, 1.5f, 1, 1.0f}};
 template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStream_t st) {
     const int64_t items = most_row_blocks(a.R, a.E, 16 * MT) * ((a.N + 15) / 16);
     const dim3 grid((unsigned)((items + 7) / 8 * 8)), threads(512);
@@ -535,17 +514,22 @@ template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStre
 template <typename T, int BLOCK> static hipError_t tiles(const Fp8Args& a, int cus, hipStream_t st) {
     typedef Fp8Gemm<T, 256, 256, 2, 4, 2, BLOCK> G256;
     typedef Fp8Gemm<T, 128, 128, 4, 2, 4, BLOCK> G128;
-    typedef Fp8Gemm<T, 128, 256, 2, 4, 2, BLOCK> W128;
+    // (a ring of three: weights that come from memory are two steps away.  8192 uneven rows in 32 groups, 4096 x 2816: 181 us with
+    // two stages, 153 with three)
+    typedef Fp8Gemm<T, 128, 256, 2, 4, 3, BLOCK> W128;
     typedef Fp8Gemm<T, 64, 128, 2, 4, 5, BLOCK> G64;
     typedef Fp8Gemm<T, 32, 128, 1, 4, 6, BLOCK> G32;
     typedef Fp8Gemm<T, 64, 64, 2, 2, 4, BLOCK> S64;
-    switch (pick_tile(kFp8, a.R, a.E, a.N, a.K, cus)) {
-        case 0: return product<G256, G128>(a, cus, 1, 0.34f, st);
-        case 1: return product<W128, G64>(a, cus, 1, 0.39f, st);
-        case 2: return product<G128, G64>(a, cus, 1, 0.64f, st);
-        case 3: return product<G64, G64>(a, cus, 1, 1.0f, st);
-        case 4: return product<G32, G32>(a, cus, 1, 1.0f, st);
-        default: return product<S64, S64>(a, cus, 2, 1.0f, st);
+    static_assert(G256::LDS_BYTES <= kLdsBesideGroups && G128::LDS_BYTES <= kLdsBesideGroups && G64::LDS_BYTES <= kLdsBesideGroups &&
+                  G32::LDS_BYTES <= kLdsBesideGroups && S64::LDS_BYTES <= kLdsBesideGroups, "only W128 leaves less than the largest tables");
+    const int i = pick_tile(kFp8, a.R, a.E, a.N, a.K, cus, a.E > kFp8Groups ? 1 : -1);
+    switch (i) {
+        case 0: return product<G256, G128>(a, kFp8[i], cus, st);
+        case 1: return product<W128, G64>(a, kFp8[i], cus, st);
+        case 2: return product<G128, G64>(a, kFp8[i], cus, st);
+        case 3: return product<G64, G64>(a, kFp8[i], cus, st);
+        case 4: return product<G32, G32>(a, kFp8[i], cus, st);
+        default: return product<S64, S64>(a, kFp8[i], cus, st);
     }
 }
 template <typename T> static hipError_t product_any(const Fp8Args& a, int cus, hipStream_t st) {

@@ -100,16 +100,17 @@ __global__ __launch_bounds__(64 * WM * WN) void grouped_weights_kernel(GroupedAr
 // Tiles, and their times for 64 k: 16384 rows in eight uneven groups, 4096 x 11008 gated, 11008 x 4096 plain, 4096 x 4096 for
 // the gradient of the input, whose operands need no transposing.  A wave's part is 128 x 64 of the largest (256 x 128 gated: 128 x 32
 // of either branch) and 32 x 32 of the small ones.
-static constexpr Tile kGated[] = {{256, 128, 1, 1.60f, 2.0f}, {128, 128, 1, 0.93f, 2.0f}, {64, 128, 1, 0.72f, 2.0f}, {32, 128, 1, 0.63f, 2.0f}, {64, 64, 2, 0.87f, 2.0f}};
-static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f}, {128, 256, 1, 0.92f, 2.0f}, {64, 256, 1, 0.67f, 2.0f},
-                                  {64, 128, 1, 0.44f, 2.0f}, {32, 128, 1, 0.37f, 2.0f}, {64, 64, 2, 0.72f, 2.0f}};
-static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f}, {128, 256, 1, 0.90f, 2.0f}, {64, 256, 1, 0.65f, 2.0f},
-                                  {64, 128, 1, 0.38f, 2.0f}, {32, 128, 1, 0.28f, 2.0f}, {64, 64, 2, 0.45f, 2.0f}};
+static constexpr Tile kGated[] = {{256, 128, 1, 1.60f, 2.0f, 4, 0.36f}, {128, 128, 1, 0.93f, 2.0f, 2, 0.76f}, {64, 128, 1, 0.72f, 2.0f, 1, 1.0f},
+                                  {32, 128, 1, 0.63f, 2.0f, 1, 1.0f}, {64, 64, 2, 0.87f, 2.0f, 1, 1.0f}};
+static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.92f, 2.0f, 4, 0.46f}, {64, 256, 1, 0.67f, 2.0f, 2, 0.64f},
+                                  {64, 128, 1, 0.44f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.37f, 2.0f, 1, 1.0f},   {64, 64, 2, 0.72f, 2.0f, 1, 1.0f}};
+static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.90f, 2.0f, 4, 0.46f}, {64, 256, 1, 0.65f, 2.0f, 2, 0.64f},
+                                  {64, 128, 1, 0.38f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.28f, 2.0f, 1, 1.0f},   {64, 64, 2, 0.45f, 2.0f, 1, 1.0f}};
 
-template <typename T, bool BCOL, bool GATED, class G, class S> static hipError_t rows(const GroupedArgs& a, int cus, int per_cu, float cost, hipStream_t st) {
+template <typename T, bool BCOL, bool GATED, class G, class S> static hipError_t rows(const GroupedArgs& a, const Tile& t, int cus, hipStream_t st) {
     const int N = BCOL ? a.N : a.K;
-    const int grid = persistent_grid(most_row_blocks(a.R, a.E, G::BM) * ((N + G::BN - 1) / G::BN), cus, per_cu);
-    hipLaunchKernelGGL((grouped_rows_kernel<T, BCOL, GATED, G, S>), dim3(grid), dim3(64 * G::NW), group_table_bytes(a.E), st, a, cost);
+    const int grid = persistent_grid(most_row_blocks(a.R, a.E, G::BM) * ((N + G::BN - 1) / G::BN), cus, t.per_cu);
+    hipLaunchKernelGGL((grouped_rows_kernel<T, BCOL, GATED, G, S>), dim3(grid), dim3(64 * G::NW), group_table_bytes(a.E), st, a, t.cost);
     return hipGetLastError();
 }
 template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hipStream_t st) {
@@ -119,12 +120,13 @@ template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hip
     typedef PairGemm<T, false, true, true, 64, 128, 2, 4, 3> G64;
     typedef PairGemm<T, false, true, true, 32, 128, 1, 4, 3> G32;
     typedef PairGemm<T, false, true, true, 64, 64, 2, 2, 3> S64;
-    switch (pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus)) {
-        case 0: return rows<T, true, true, G256, Q256>(a, cus, 1, 0.36f, st);
-        case 1: return rows<T, true, true, G128, G64>(a, cus, 1, 0.76f, st);
-        case 2: return rows<T, true, true, G64, G64>(a, cus, 1, 1.0f, st);
-        case 3: return rows<T, true, true, G32, G32>(a, cus, 1, 1.0f, st);
-        default: return rows<T, true, true, S64, S64>(a, cus, 2, 1.0f, st);
+    const int i = pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus);
+    switch (i) {
+        case 0: return rows<T, true, true, G256, Q256>(a, kGated[i], cus, st);
+        case 1: return rows<T, true, true, G128, G64>(a, kGated[i], cus, st);
+        case 2: return rows<T, true, true, G64, G64>(a, kGated[i], cus, st);
+        case 3: return rows<T, true, true, G32, G32>(a, kGated[i], cus, st);
+        default: return rows<T, true, true, S64, S64>(a, kGated[i], cus, st);
     }
 }
 template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, int cus, hipStream_t st) {
@@ -135,13 +137,15 @@ template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, i
     typedef PairGemm<T, false, BCOL, false, 64, 128, 2, 4, 4> G64;
     typedef PairGemm<T, false, BCOL, false, 32, 128, 1, 4, 4> G32;
     typedef PairGemm<T, false, BCOL, false, 64, 64, 2, 2, 4> S64;
-    switch (BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus)) {
-        case 0: return rows<T, BCOL, false, G256, Q256>(a, cus, 1, 0.38f, st);
-        case 1: return rows<T, BCOL, false, G128, G64>(a, cus, 1, 0.46f, st);
-        case 2: return rows<T, BCOL, false, W64, G64>(a, cus, 1, 0.64f, st);
-        case 3: return rows<T, BCOL, false, G64, G64>(a, cus, 1, 1.0f, st);
-        case 4: return rows<T, BCOL, false, G32, G32>(a, cus, 1, 1.0f, st);
-        default: return rows<T, BCOL, false, S64, S64>(a, cus, 2, 1.0f, st);
+    const int i = BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus);
+    const Tile& t = BCOL ? kPlain[i] : kInput[i];
+    switch (i) {
+        case 0: return rows<T, BCOL, false, G256, Q256>(a, t, cus, st);
+        case 1: return rows<T, BCOL, false, G128, G64>(a, t, cus, st);
+        case 2: return rows<T, BCOL, false, W64, G64>(a, t, cus, st);
+        case 3: return rows<T, BCOL, false, G64, G64>(a, t, cus, st);
+        case 4: return rows<T, BCOL, false, G32, G32>(a, t, cus, st);
+        default: return rows<T, BCOL, false, S64, S64>(a, t, cus, st);
     }
 }
 hipError_t launch_grouped_forward(int dtype, const GroupedArgs& a, int cus, hipStream_t st) {

@@ -146,25 +146,38 @@ inline int persistent_grid(int64_t items, int cus, int per_cu) {
 }
 
 // A tile that a kernel is built for, and what an item of it takes: `step` us for each 128 bytes of the contraction, measured
-// with every CU at work on `per_cu` items of a large problem, and `fixed` us beside them.
+// with every CU at work on `per_cu` items of a large problem, and `fixed` us beside them.  Left-over items are done in `parts`
+// parts of `cost` of an item's time (whole_items; 1: they are not).
 struct Tile {
     int bm, bn, per_cu;
     float step, fixed;
+    int parts;
+    float cost;
 };
 // The tile whose rounds of items take the least time.  Where the boundaries are known on the device alone, every group
-// is taken to have the average number of rows and half a block more.
-template <int N> int pick_tile(const Tile (&tiles)[N], int64_t R, int64_t E, int64_t cols, int64_t bytes, int cus) {
-    int best = 0;
+// is taken to have the average number of rows and half a block more, and the last round to be as full as rounds are on average.
+template <int N> int pick_tile(const Tile (&tiles)[N], int64_t R, int64_t E, int64_t cols, int64_t bytes, int cus, int without = -1) {
+    int best = -1;
     double least = 0.0;
     for (int i = 0; i < N; ++i) {
+        if (i == without) continue;
         const Tile& t = tiles[i];
         const double groups = (double)(R < E ? R : E), mean = R / groups;
         const double blocks = E == 1 ? (double)((R + t.bm - 1) / t.bm) : mean <= 1.0 ? groups : groups * (mean / t.bm + 0.5 > 1.0 ? mean / t.bm + 0.5 : 1.0);
         const double per_cu = blocks * (double)((cols + t.bn - 1) / t.bn) / cus, x = per_cu / t.per_cu;
-        const double rounds = x <= 1.0 ? 1.0 : E == 1 ? (double)(int64_t)(x + 0.999) : x + 0.5;
+        double rounds = 1.0;
+        if (x > 1.0) {
+            const int64_t whole = (int64_t)x;
+            double last = x > whole ? 1.0 : 0.0;
+            if (t.parts > 1 && x > whole) {
+                const double split = (double)(int64_t)((x - whole) * t.parts + 0.999) * t.cost;
+                if (split < 0.95) last = split;
+            }
+            rounds = E == 1 ? whole + last : x + (t.parts == 4 ? 0.28 : t.parts == 2 ? 0.32 : 0.5);
+        }
         const double alone = per_cu <= 1.0 && t.per_cu > 1 ? 0.6 : 1.0;   // an item that has a CU to itself is done sooner
         const double time = rounds * (t.fixed + t.step * alone * (double)((bytes + 127) / 128));
-        if (i == 0 || time < least) { best = i; least = time; }
+        if (best < 0 || time < least) { best = i; least = time; }
     }
     return best;
 }

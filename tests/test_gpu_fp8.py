@@ -212,3 +212,22 @@ def test_a_training_step_in_8_bits(M, K, N):
         for out, a, b in ((Y, X.double(), W.double()), (dX, dY.double(), W.double().t()), (dW, X.double().t(), dY.double())):
             slack = (a.abs() @ b.abs()) * (2 * 2.0 ** -4 + 2.0 ** -8 + 2.0 ** -7) + a.abs().max() * b.abs().max() * a.shape[1] * 2 * 2.0 ** -16
             assert bool(((out.double() - a @ b).abs() <= slack).all())
+
+
+def test_more_groups_than_the_largest_ring_leaves_room_for():
+    """1024 groups, whose tables take more LDS than the tile with the deepest ring leaves."""
+    gen, E, K, N = torch.Generator().manual_seed(27), 1024, 144, 520
+    sizes = [(5 * i) % 7 for i in range(E)]
+    sizes[700] = 900
+    R = sum(sizes)
+    A, sa = _operand(gen, R, K, 1)
+    B, sb = torch.randint(0, 0x70, (E, N, K), generator=gen, dtype=torch.uint8).cuda().view(u.E4M3), torch.rand((E, 2, 5), generator=gen).cuda()
+    Y = torch.full((R, N), float("nan"), dtype=BF16, device="cuda")
+    ff.ffuse_grouped_gemm_fp8(ff.DT_BF16, A, sa, B, sb, u.offsets_of(sizes), Y)
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(Y).all())
+    starts = [sum(sizes[:i]) for i in range(E)]
+    for e in (0, 1, 63, 64, 65, 500, 700, 1022, 1023):
+        a, n = starts[e], sizes[e]
+        if n:
+            _check_product(Y[a:a + n], A[a:a + n], sa[:, a:a + n], B[e], sb[e], 128, BF16, f"group {e}")
