@@ -448,11 +448,11 @@ template <typename T, int BLOCK> __global__ __launch_bounds__(256) void quantize
 }
 
 // The transpose: a workgroup turns 128 rows x 128 columns of X into 128 bytes of 128 rows of Q, through LDS.  A thread
-// takes 64 rows of one column.
+// takes 32 rows of two neighbouring columns, one LDS read for both.
 template <typename T, int BLOCK> __global__ __launch_bounds__(256) void quantize_columns_kernel(QuantArgs a) {
     constexpr int PITCH = 272;   // bytes of a row in LDS: 16-byte writes, and columns read by neighbouring lanes
     __shared__ __attribute__((aligned(16))) char tile[128 * PITCH];
-    __shared__ uint32_t most[256];
+    __shared__ uint2 most[256];
     const int tid = threadIdx.x;
     const int64_t kb = blockIdx.x % a.nk, mb = blockIdx.x / a.nk, m0 = 128 * mb, k0 = 128 * kb;
 #pragma unroll
@@ -463,34 +463,63 @@ template <typename T, int BLOCK> __global__ __launch_bounds__(256) void quantize
         *reinterpret_cast<u32x4*>(tile + r * PITCH + 2 * c) = w;
     }
     __syncthreads();
-    const int c = tid & 127, half = tid >> 7;
-    const char* col = tile + 64 * half * PITCH + 2 * c;
-    uint32_t top = 0;
-    for (int r = 0; r < 64; ++r) top = max(top, finite_magnitude((float)*reinterpret_cast<const T*>(col + r * PITCH)));
-    if constexpr (BLOCK == 128) {
+    const int pair = tid & 63, quarter = tid >> 6;
+    const char* from = tile + 32 * quarter * PITCH + 4 * pair;
+    uint32_t w[32];
+    uint2 top = {0, 0};
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    for (int r = 0; r < 32; ++r) {
+        w[r] = *reinterpret_cast<const uint32_t*>(from + r * PITCH);
+        float lo, hi;
+        unpack2<T>(w[r], lo, hi);
+        top.x = max(top.x, finite_magnitude(lo));
+        top.y = max(top.y, finite_magnitude(hi));
+    }
+    if constexpr (BLOCK == 128) {
+        top.x = max(top.x, top.y);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) top.x = max(top.x, (uint32_t)__shfl_xor((int)top.x, d));
+        top.y = top.x;
     }
     most[tid] = top;
     __syncthreads();
-    if constexpr (BLOCK == 128) top = max(max(most[0], most[64]), max(most[128], most[192]));
-    else top = max(most[c], most[128 + c]);
-    const float s = block_scale(top), inv = inverse_of_power(s);
-    if (BLOCK == 128 ? tid == 0 : (half == 0 && k0 + c < a.K)) a.scale[mb * a.ns + (BLOCK == 128 ? kb : k0 + c)] = s;
-    if (k0 + c >= a.K) return;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int64_t m = m0 + 64 * half + 16 * u;
-        if (m >= a.ld) break;
-        u32x4 o;
+    for (int q = 0; q < 4; ++q) {
+        top.x = max(top.x, most[64 * q + pair].x);
+        top.y = max(top.y, most[64 * q + pair].y);
+    }
+    const int64_t k = k0 + 2 * pair;
+    const float s[2] = {block_scale(top.x), block_scale(top.y)};
+    if (BLOCK == 128 ? tid == 0 : (quarter == 0 && k < a.K)) {
+        a.scale[mb * a.ns + (BLOCK == 128 ? kb : k)] = s[0];
+        if (BLOCK == 1) a.scale[mb * a.ns + k + 1] = s[1];
+    }
+    // the numbers go back through LDS (everybody has read the tile), so that rows of Q leave in whole lines
+    constexpr int QP = 144;
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            float v[4];
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (float)*reinterpret_cast<const T*>(col + (16 * u + 4 * d + i) * PITCH);
-            o[d] = to_e4m3(v, inv);
+        for (int c = 0; c < 2; ++c) {
+            const float inv = inverse_of_power(s[c]);
+            u32x4 o;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float lo, hi;
+                    unpack2<T>(w[16 * u + 4 * d + i], lo, hi);
+                    v[i] = c ? hi : lo;
+                }
+                o[d] = to_e4m3(v, inv);
+            }
+            *reinterpret_cast<u32x4*>(tile + (2 * pair + c) * QP + 32 * quarter + 16 * u) = o;
         }
-        *reinterpret_cast<u32x4*>(a.Q + (k0 + c) * a.ld + m) = o;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        const int r = 32 * p + (tid >> 3), at = 16 * (tid & 7);
+        if (k0 + r < a.K && m0 + at < a.ld) *reinterpret_cast<u32x4*>(a.Q + (k0 + r) * a.ld + m0 + at) = *reinterpret_cast<const u32x4*>(tile + r * QP + at);
     }
 }
 

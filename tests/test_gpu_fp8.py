@@ -231,3 +231,25 @@ def test_more_groups_than_the_largest_ring_leaves_room_for():
         a, n = starts[e], sizes[e]
         if n:
             _check_product(Y[a:a + n], A[a:a + n], sa[:, a:a + n], B[e], sb[e], 128, BF16, f"group {e}")
+
+
+@pytest.mark.parametrize("M,K,N", [(4500, 272, 8200), (1300, 4096, 4104), (1300, 4096, 6000), (700, 528, 5000), (33, 2064, 9000), (20, 4096, 2056)])
+@pytest.mark.parametrize("block", (1, 128))
+def test_products_of_many_tiles(M, K, N, block):
+    """More tiles than the device has CUs, and the rests of their rounds: every column of the rows at the edges of
+    tiles, and of some others."""
+    gen = torch.Generator().manual_seed(28)
+    A, sa = _operand(gen, M, K, 1)
+    B, sb = _operand(gen, N, K, block)
+    Y = torch.full((M, N), float("nan"), dtype=BF16, device="cuda")
+    print("many tiles", M, K, N, block, flush=True)
+    ff.ffuse_gemm_fp8(ff.DT_BF16, A, sa, B, sb, Y)
+    torch.cuda.synchronize()
+    assert bool(torch.isfinite(Y).all())
+    rows = sorted({r for at in range(0, M + 1, 64) for r in (at - 1, at) if 0 <= r < M} | {M - 1})
+    rows = rows if len(rows) < 48 else rows[:24] + rows[-24:]
+    for cols in (slice(0, 2100), slice(max(0, N - 2100), N)):
+        first = cols.start // 128 if block == 128 else cols.start
+        if block == 128 and cols.start % 128:
+            cols = slice(first * 128, N)
+        _check_product(Y[rows, cols], A[rows], sa[:, rows], B[cols], sb[:, first:first + (cols.stop - cols.start + block - 1) // block], block, BF16, f"{M} x {K} x {N}")

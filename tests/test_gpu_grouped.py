@@ -329,3 +329,43 @@ def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
     finally:
         ff.ffuse_force_plan(None)
         ff.ffuse_set_workspace(None)
+
+
+@pytest.mark.parametrize("sizes,K,N,gated", [
+    ([9000, 300, 0, 10700], 136, 4104, False),      # 256 x 256 tiles, several rounds and a rest that is done in parts
+    ([9000, 300, 0, 10700], 72, 2056, True),
+    ([100] * 23 + [57], 1000, 2056, False),         # 128 x 256, a little over a round
+    ([130, 40, 200, 0, 255, 129, 128, 90] * 8, 520, 1416, True),
+    ([60, 10, 64, 65, 3] * 20, 264, 2056, False),
+])
+def test_forward_and_gradients_of_many_tiles(sizes, K, N, gated):
+    """Products of more tiles than the device has CUs, checked in every element: the rests of the rounds, too."""
+    gen, R, E, t = torch.Generator().manual_seed(15), sum(sizes) + 2, len(sizes), BF16
+    X, W, dY = u.normal(gen, (R, K), 1.0, t), u.normal(gen, (E, K, N), K ** -0.5, t), u.normal(gen, (R, N), 0.1, t)
+    W3 = u.normal(gen, (E, K, N), K ** -0.5, t) if gated else None
+    off = u.offsets_of(sizes)
+    Y, dX, dW = (torch.full(s, 7.0, dtype=t, device="cuda") for s in ((R, N), (R, K), (E, K, N)))
+    print("many tiles", len(sizes), R, K, N, gated, flush=True)
+    ff.ffuse_grouped_gemm(ff.DT_BF16, X, W, W3, off, ff.ACT_SILU if gated else ff.ACT_IDENTITY, Y)
+    ff.ffuse_grouped_gemm_dx(ff.DT_BF16, dY, W, off, dX)
+    ff.ffuse_grouped_gemm_dw(ff.DT_BF16, X, dY, off, dW)
+    torch.cuda.synchronize()
+    for e, s in _spans(sizes):
+        want, err = u.product64(X[s], W[e], None if W3 is None else W3[e], ff.ACT_SILU if gated else ff.ACT_IDENTITY, t)
+        u.assert_within(Y[s], want, err, f"Y, group {e}")
+        want, err = u.mm(dY[s], W[e].t())
+        u.assert_within(dX[s], want, u.rounded(want, err, t), f"dX, group {e}")
+        want, err = u.mm(X[s].t(), dY[s])
+        u.assert_within(dW[e], want, u.rounded(want, err, t), f"dW, group {e}")
+    assert bool((Y[R - 2:] == 7).all()) and bool((dX[R - 2:] == 7).all())
+
+
+def test_weight_gradient_of_large_blocks():
+    gen, sizes, K, N = torch.Generator().manual_seed(16), [700, 0, 1301, 64], 1032, 2056
+    R = sum(sizes)
+    X, dY = u.normal(gen, (R, K), 1.0, F16), u.normal(gen, (R, N), 0.1, F16)
+    dW = torch.full((len(sizes), K, N), float("nan"), dtype=F16, device="cuda")
+    ff.ffuse_grouped_gemm_dw(ff.DT_F16, X, dY, u.offsets_of(sizes), dW)
+    for e, s in _spans(sizes):
+        want, err = u.mm(X[s].t(), dY[s])
+        u.assert_within(dW[e], want, u.rounded(want, err, F16), f"group {e}")
