@@ -91,9 +91,9 @@ __global__ __launch_bounds__(64 * WM * WN) void grouped_weights_kernel(GroupedAr
     c.b[0].aim(static_cast<const char*>(a.W) + ((int64_t)first * a.N + n0) * 2, a.N, a.N - n0, c.K, wave, lane);
     G::fill(smem, c);
     G::run(smem, c, acc, false);
+    lds_loads_in_flight_at_most<0>();   // (loads past the last stage write to LDS, if only zeros: not after the workgroup is gone)
     char* dW = static_cast<char*>(a.C) + ((int64_t)e * a.K * a.N + (int64_t)m0 * a.N + n0) * 2;
     G::template store<ACT_IDENTITY>(smem, acc, dW, (uint32_t)a.N, a.K - m0, a.N - n0, wave);
-    lds_loads_in_flight_at_most<0>();   // (loads past the last stage write to LDS, if only zeros: not after the workgroup is gone)
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------

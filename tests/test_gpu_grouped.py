@@ -369,3 +369,22 @@ def test_weight_gradient_of_large_blocks():
     for e, s in _spans(sizes):
         want, err = u.mm(X[s].t(), dY[s])
         u.assert_within(dW[e], want, u.rounded(want, err, F16), f"group {e}")
+
+
+def test_as_many_groups_as_a_call_takes():
+    """1024 groups of about a hundred rows: the largest boundary tables beside the deepest rings."""
+    gen, E, K, N = torch.Generator().manual_seed(17), 1024, 72, 2056
+    sizes = [(37 * i) % 200 for i in range(E)]
+    R = sum(sizes)
+    X, dY, W = torch.randn(R, K, device="cuda").to(BF16), torch.randn(R, N, device="cuda").to(BF16), (torch.randn(E, K, N, device="cuda") * K ** -0.5).to(BF16)
+    off, Y, dX, dW = u.offsets_of(sizes), torch.empty((R, N), dtype=BF16, device="cuda"), torch.empty((R, K), dtype=BF16, device="cuda"), torch.empty_like(W)
+    ff.ffuse_grouped_gemm(ff.DT_BF16, X, W, None, off, ff.ACT_IDENTITY, Y)
+    ff.ffuse_grouped_gemm_dx(ff.DT_BF16, dY, W, off, dX)
+    ff.ffuse_grouped_gemm_dw(ff.DT_BF16, X, dY, off, dW)
+    torch.cuda.synchronize()
+    for e, s in _spans(sizes):
+        if e % 41 and e not in (1, 63, 64, 1022, 1023):
+            continue
+        for got, (want, err) in ((Y[s], u.mm(X[s], W[e])), (dX[s], u.mm(dY[s], W[e].t())), (dW[e], u.mm(X[s].t(), dY[s]))):
+            u.assert_within(got, want, u.rounded(want, err, BF16), f"group {e}")
+    assert bool(torch.isfinite(Y).all()) and bool(torch.isfinite(dX).all()) and bool(torch.isfinite(dW).all())
