@@ -5,6 +5,7 @@ import torch
 
 from paper_2512_12949_amd import binding as ff
 
+import gpu_util as gu
 import grouped_util as u
 
 pytestmark = pytest.mark.gpu
@@ -308,6 +309,7 @@ def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
                 grouped()
         torch.cuda.synchronize()
     if registered and not in_graph:
+        gu.Workspace.buf = None      # (the other tests' registered one)
         ff.ffuse_set_workspace(ws)
     A, B1, B2 = u.normal(gen, (100, 136), 1.0, BF16), u.normal(gen, (136, 264), 136 ** -0.5, BF16), u.normal(gen, (264, 72), 264 ** -0.5, BF16)
     h, eh = u.product64(A, B1, None, ff.ACT_RELU, BF16)
@@ -328,7 +330,8 @@ def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
                 torch.cuda.synchronize()
     finally:
         ff.ffuse_force_plan(None)
-        ff.ffuse_set_workspace(None)
+        if registered and not in_graph:
+            ff.ffuse_set_workspace(None)
 
 
 @pytest.mark.parametrize("sizes,K,N,gated", [
