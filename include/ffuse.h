@@ -258,8 +258,8 @@ int ffuse_grouped_ffn(int dtype, const void* X, const void* W1, const void* W3 /
  *      magnitude of the block to 448 or below (1 for a block of zeros): dividing by it is exact, the quotient is rounded once, to nearest
  *      even.  Infinities and NaN do not count for the scale and become NaN.  M >= 0, K a multiple of 8 up to 2^20.
  *   ffuse_gemm_fp8       Y[m][n] = sum over blocks b of sa[b][m] sb[b][n / b_block] (sum over k in b of A[m][k] B[n][k])
- *      A[M][K], B[N][K] in e4m3, scales in fp32 (any, not only powers of two) laid out as above, b_block 1 or 128, Y[M][N] of
- *      type dtype (bf16 or fp16), rounded once.  M >= 0, K a multiple of 16, N of 8.  An inference product has A = rows of
+ *      A[M][K], B[N][K] in e4m3, scales in fp32 (any, not only powers of two; sa sb is taken first) laid out as above, b_block 1
+ *      or 128, Y[M][N] of type dtype (bf16 or fp16), rounded once.  M >= 0, K a multiple of 16, N of 8.  An inference product has A = rows of
  *      X by 1 x 128 and B = W^T by 128 x 128; its gradients dX = dY W^T (B = W untransposed) and dW = X^T dY (both
  *      operands transposed, by 1 x 128) are this product too.
  *   ffuse_grouped_gemm_fp8   the same with the rows of A grouped by expert as above: B[E][N][K], sb[E][ceil(K/128)][...]. -- */
