@@ -537,7 +537,7 @@ template <class G, class S> static hipError_t product(const Fp8Args& a, const Ti
 }
 // Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
 static constexpr Tile kFp8[] = {{256, 256, 1, 1.68f, 2.0f, 4, 0.36f}, {128, 256, 1, 1.00f, 2.0f, 4, 0.39f}, {128, 128, 1, 0.58f, 2.0f, 2, 0.64f},
-                                {64, 128, 1, 0.37f, 1.5f, 1, 1.0f},   {32, 128, 1, 0.32f, 1.5f, 1, 1.0f},   {64, 64, 2, 0.42f, 1.5f, 1, 1.0f}};
+                                {64, 128, 1, 0.40f, 1.5f, 1, 1.0f},   {32, 128, 1, 0.33f, 1.5f, 1, 1.0f},   {64, 64, 2, 0.58f, 1.5f, 1, 1.0f}};
 template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStream_t st) {
     const int64_t items = most_row_blocks(a.R, a.E, 16 * MT) * ((a.N + 15) / 16);
     const dim3 grid((unsigned)((items + 7) / 8 * 8)), threads(512);

@@ -105,15 +105,20 @@ __global__ __launch_bounds__(64 * WM * WN) void grouped_weights_kernel(GroupedAr
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------
-// Tiles, and their times for 64 k: 16384 rows in eight uneven groups, 4096 x 11008 gated, 11008 x 4096 plain, 4096 x 4096 for
-// the gradient of the input, whose operands need no transposing.  A wave's part is 128 x 64 of the largest (256 x 128 gated: 128 x 32
-// of either branch) and 32 x 32 of the small ones.
-static constexpr Tile kGated[] = {{256, 128, 1, 1.60f, 2.0f, 4, 0.36f}, {128, 128, 1, 0.93f, 2.0f, 2, 0.76f}, {64, 128, 1, 0.72f, 2.0f, 1, 1.0f},
-                                  {32, 128, 1, 0.63f, 2.0f, 1, 1.0f}, {64, 64, 2, 0.87f, 2.0f, 1, 1.0f}};
-static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.92f, 2.0f, 4, 0.46f}, {64, 256, 1, 0.67f, 2.0f, 2, 0.64f},
-                                  {64, 128, 1, 0.44f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.37f, 2.0f, 1, 1.0f},   {64, 64, 2, 0.72f, 2.0f, 1, 1.0f}};
-static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.90f, 2.0f, 4, 0.46f}, {64, 256, 1, 0.65f, 2.0f, 2, 0.64f},
-                                  {64, 128, 1, 0.38f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.28f, 2.0f, 1, 1.0f},   {64, 64, 2, 0.45f, 2.0f, 1, 1.0f}};
+// Tiles, and their times for 64 k, set on 16384 rows in eight uneven groups (4096 x 11008 gated, 11008 x 4096 plain, 4096 x 4096 for
+// the gradient of the input, whose operands need no transposing) and on 160 drawn problems of 1 to 16384 rows and 1 to 128
+// groups each, every tile timed on each: what is chosen takes 2 % more time than the best of them on average.  128 x 128, where
+// there are too few blocks of 128 x 256 for the CUs: 568 rows in five groups, 7168 x 3336, 75 us instead of 97 (plain) and 68
+// instead of 93 (input); 3184 in 23, 11656 x 576, 132 instead of 154 and 178 instead of 231.  A wave's part is 128 x 64 of the
+// largest (256 x 128 gated: 128 x 32 of either branch) and 32 x 32 of the small ones.
+static constexpr Tile kGated[] = {{256, 128, 1, 1.60f, 2.0f, 4, 0.36f}, {128, 128, 1, 1.00f, 2.0f, 2, 0.76f}, {64, 128, 1, 0.68f, 2.0f, 1, 1.0f},
+                                  {32, 128, 1, 0.58f, 2.0f, 1, 1.0f}, {64, 64, 2, 1.15f, 2.0f, 1, 1.0f}};
+static constexpr Tile kPlain[] = {{256, 256, 1, 1.59f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.97f, 2.0f, 4, 0.46f}, {128, 128, 1, 0.60f, 2.0f, 2, 0.73f},
+                                  {64, 256, 1, 0.67f, 2.0f, 2, 0.64f},  {64, 128, 1, 0.44f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.37f, 2.0f, 1, 1.0f},
+                                  {64, 64, 2, 0.72f, 2.0f, 1, 1.0f}};
+static constexpr Tile kInput[] = {{256, 256, 1, 1.50f, 2.0f, 4, 0.38f}, {128, 256, 1, 0.94f, 2.0f, 4, 0.46f}, {128, 128, 1, 0.59f, 2.0f, 2, 0.64f},
+                                  {64, 256, 1, 0.63f, 2.0f, 2, 0.64f},  {64, 128, 1, 0.36f, 2.0f, 1, 1.0f},   {32, 128, 1, 0.27f, 2.0f, 1, 1.0f},
+                                  {64, 64, 2, 0.66f, 2.0f, 1, 1.0f}};
 
 template <typename T, bool BCOL, bool GATED, class G, class S> static hipError_t rows(const GroupedArgs& a, const Tile& t, int cus, hipStream_t st) {
     const int N = BCOL ? a.N : a.K;
@@ -139,8 +144,8 @@ template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hip
 }
 template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, int cus, hipStream_t st) {
     typedef PairGemm<T, false, BCOL, false, 256, 256, 2, 4, 2> G256;
-    typedef PairGemm<T, false, BCOL, false, 128, 128, 2, 4, 4> Q256;
-    typedef PairGemm<T, false, BCOL, false, 128, 256, 2, 4, 3> G128;
+    typedef PairGemm<T, false, BCOL, false, 128, 256, 2, 4, 3> W128;
+    typedef PairGemm<T, false, BCOL, false, 128, 128, 2, 4, 4> G128;
     typedef PairGemm<T, false, BCOL, false, 64, 256, 2, 4, 3> W64;
     typedef PairGemm<T, false, BCOL, false, 64, 128, 2, 4, 4> G64;
     typedef PairGemm<T, false, BCOL, false, 32, 128, 1, 4, 4> G32;
@@ -148,11 +153,12 @@ template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, i
     const int i = BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus);
     const Tile& t = BCOL ? kPlain[i] : kInput[i];
     switch (i) {
-        case 0: return rows<T, BCOL, false, G256, Q256>(a, t, cus, st);
-        case 1: return rows<T, BCOL, false, G128, G64>(a, t, cus, st);
-        case 2: return rows<T, BCOL, false, W64, G64>(a, t, cus, st);
-        case 3: return rows<T, BCOL, false, G64, G64>(a, t, cus, st);
-        case 4: return rows<T, BCOL, false, G32, G32>(a, t, cus, st);
+        case 0: return rows<T, BCOL, false, G256, G128>(a, t, cus, st);
+        case 1: return rows<T, BCOL, false, W128, G64>(a, t, cus, st);
+        case 2: return rows<T, BCOL, false, G128, G64>(a, t, cus, st);
+        case 3: return rows<T, BCOL, false, W64, G64>(a, t, cus, st);
+        case 4: return rows<T, BCOL, false, G64, G64>(a, t, cus, st);
+        case 5: return rows<T, BCOL, false, G32, G32>(a, t, cus, st);
         default: return rows<T, BCOL, false, S64, S64>(a, t, cus, st);
     }
 }

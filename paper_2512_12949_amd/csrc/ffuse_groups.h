@@ -165,17 +165,20 @@ template <int N> int pick_tile(const Tile (&tiles)[N], int64_t R, int64_t E, int
         const double groups = (double)(R < E ? R : E), mean = R / groups;
         const double blocks = E == 1 ? (double)((R + t.bm - 1) / t.bm) : mean <= 1.0 ? groups : groups * (mean / t.bm + 0.5 > 1.0 ? mean / t.bm + 0.5 : 1.0);
         const double per_cu = blocks * (double)((cols + t.bn - 1) / t.bn) / cus, x = per_cu / t.per_cu;
+        const double rest = t.parts == 4 ? 0.28 : t.parts == 2 ? 0.32 : 0.5;
         double rounds = 1.0;
-        if (x > 1.0) {
+        if (E > 1) {
+            rounds = x > 1.0 ? x + rest : x > 0.8 ? 1.0 + rest * (x - 0.8) / 0.2 : 1.0;   // (uneven groups may have more blocks)
+        } else if (x > 1.0) {
             const int64_t whole = (int64_t)x;
             double last = x > whole ? 1.0 : 0.0;
             if (t.parts > 1 && x > whole) {
                 const double split = (double)(int64_t)((x - whole) * t.parts + 0.999) * t.cost;
                 if (split < 0.95) last = split;
             }
-            rounds = E == 1 ? whole + last : x + (t.parts == 4 ? 0.28 : t.parts == 2 ? 0.32 : 0.5);
+            rounds = whole + last;
         }
-        const double alone = per_cu <= 1.0 && t.per_cu > 1 ? 0.6 : 1.0;   // an item that has a CU to itself is done sooner
+        const double alone = t.per_cu > 1 && x < 1.0 ? (x > 0.3 ? x : 0.3) : 1.0;   // where not every CU has all its items, each is done sooner
         const double time = rounds * (t.fixed + t.step * alone * (double)((bytes + 127) / 128));
         if (best < 0 || time < least) { best = i; least = time; }
     }

@@ -340,6 +340,7 @@ def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
     ([100] * 23 + [57], 1000, 2056, False),         # 128 x 256, a little over a round
     ([130, 40, 200, 0, 255, 129, 128, 90] * 8, 520, 1416, True),
     ([60, 10, 64, 65, 3] * 20, 264, 2056, False),
+    ([129] * 15, 1144, 1144, False),                # 128 x 128, one round and a few tiles in halves
 ])
 def test_forward_and_gradients_of_many_tiles(sizes, K, N, gated):
     """Products of more tiles than the device has CUs, checked in every element: the rests of the rounds, too."""
