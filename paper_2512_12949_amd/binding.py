@@ -180,7 +180,8 @@ def _addr(t):
 _raw_stream = None
 
 
-def _stream_addr(stream):
+def _stream_addr(stream, device=None):
+    """The handle of `stream`, or of the current one of the current device (`device`, where the caller knows it)."""
     if stream is not None:
         return int(stream)
     global _raw_stream
@@ -188,10 +189,10 @@ def _stream_addr(stream):
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         if raw is None:
-            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
+            _raw_stream = lambda device: torch.cuda.current_stream().cuda_stream
         else:
-            _raw_stream = lambda: raw(torch.cuda.current_device())
-    return _raw_stream()
+            _raw_stream = lambda device: raw(torch.cuda.current_device() if device is None else device)
+    return _raw_stream(device)
 
 
 def _call(name, X, W1, W3, W2, act, Y, stream, check):
@@ -439,19 +440,23 @@ def ffuse_conv_chain_f16(X, W1, W2, act, Y, stream=None, check=True):
 # an attribute or two.)
 
 _torch = None
-_has_device = False
+_device = None        # () -> the current device
 
 
 def _tensors(dtype):
     """torch, the operands' type and the current device."""
-    global _torch, _has_device
+    global _torch, _device
     if _torch is None:
         import torch
-        _has_device = torch.cuda.is_available()
+        if torch.cuda.is_available():
+            torch.cuda.current_device()        # (the first one sets the device up)
+            _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        else:
+            _device = lambda: -2
         _torch = torch
     if dtype != DT_BF16 and dtype != DT_F16:
         raise ValueError(f"dtype {dtype}: DT_BF16 or DT_F16")
-    return _torch, _torch.bfloat16 if dtype == DT_BF16 else _torch.float16, _torch.cuda.current_device() if _has_device else -2
+    return _torch, _torch.bfloat16 if dtype == DT_BF16 else _torch.float16, _device()
 
 
 def _want(device, name, t, shape, dtype):
@@ -488,7 +493,7 @@ def ffuse_grouped_gemm(dtype, X, W, W3, offsets, act, Y, stream=None, check=True
     _want(dev, "offsets", offsets, (E + 1,), torch.int32)
     _want(dev, "Y", Y, (R, N), t)
     return _rc("ffuse_grouped_gemm", (_lib or lib()).ffuse_grouped_gemm(dtype, X.data_ptr(), W.data_ptr(), _addr(W3), offsets.data_ptr(), int(act), R, E, K, N,
-                                                                        Y.data_ptr(), _stream_addr(stream)), check)
+                                                                        Y.data_ptr(), _stream_addr(stream, dev)), check)
 
 
 def ffuse_grouped_gemm_dx(dtype, dY, W, offsets, dX, stream=None, check=True):
@@ -500,7 +505,7 @@ def ffuse_grouped_gemm_dx(dtype, dY, W, offsets, dX, stream=None, check=True):
     _want(dev, "offsets", offsets, (E + 1,), torch.int32)
     _want(dev, "dX", dX, (R, K), t)
     return _rc("ffuse_grouped_gemm_dx", (_lib or lib()).ffuse_grouped_gemm_dx(dtype, dY.data_ptr(), W.data_ptr(), offsets.data_ptr(), R, E, K, N, dX.data_ptr(),
-                                                                              _stream_addr(stream)), check)
+                                                                              _stream_addr(stream, dev)), check)
 
 
 def ffuse_grouped_gemm_dw(dtype, X, dY, offsets, dW, stream=None, check=True):
@@ -512,7 +517,7 @@ def ffuse_grouped_gemm_dw(dtype, X, dY, offsets, dW, stream=None, check=True):
     _want(dev, "offsets", offsets, (E + 1,), torch.int32)
     _want(dev, "dW", dW, (E, K, N), t)
     return _rc("ffuse_grouped_gemm_dw", (_lib or lib()).ffuse_grouped_gemm_dw(dtype, X.data_ptr(), dY.data_ptr(), offsets.data_ptr(), R, E, K, N, dW.data_ptr(),
-                                                                              _stream_addr(stream)), check)
+                                                                              _stream_addr(stream, dev)), check)
 
 
 def ffuse_grouped_workspace_bytes(dtype, R, N1) -> int:
@@ -536,7 +541,7 @@ def ffuse_grouped_ffn(dtype, X, W1, W3, W2, offsets, act, Y, workspace, stream=N
         _want(dev, "workspace", workspace, workspace.shape, workspace.dtype)
         nbytes = workspace.numel() * workspace.element_size()
     return _rc("ffuse_grouped_ffn", (_lib or lib()).ffuse_grouped_ffn(dtype, X.data_ptr(), W1.data_ptr(), _addr(W3), W2.data_ptr(), offsets.data_ptr(), int(act),
-                                                                      R, E, K, N1, N2, Y.data_ptr(), _addr(workspace), nbytes, _stream_addr(stream)), check)
+                                                                      R, E, K, N1, N2, Y.data_ptr(), _addr(workspace), nbytes, _stream_addr(stream, dev)), check)
 
 
 def ffuse_fp8_quantize(dtype, X, Q, scale, block_rows=1, transpose=False, stream=None, check=True):
@@ -549,7 +554,7 @@ def ffuse_fp8_quantize(dtype, X, Q, scale, block_rows=1, transpose=False, stream
     _want(dev, "Q", Q, (m, (k + 15) // 16 * 16), torch.float8_e4m3fn)
     _want(dev, "scale", scale, ((k + 127) // 128, (m + 127) // 128 if block_rows == 128 else m), torch.float32)
     return _rc("ffuse_fp8_quantize", (_lib or lib()).ffuse_fp8_quantize(dtype, X.data_ptr(), M, K, int(block_rows), 1 if transpose else 0, Q.data_ptr(),
-                                                                        scale.data_ptr(), _stream_addr(stream)), check)
+                                                                        scale.data_ptr(), _stream_addr(stream, dev)), check)
 
 
 def _fp8_block(sb, kb, N):
@@ -574,7 +579,7 @@ def ffuse_gemm_fp8(dtype, A, sa, B, sb, Y, stream=None, check=True):
     _want(dev, "sb", sb, (kb, (N + block - 1) // block), torch.float32)
     _want(dev, "Y", Y, (M, N), t)
     return _rc("ffuse_gemm_fp8", (_lib or lib()).ffuse_gemm_fp8(dtype, A.data_ptr(), sa.data_ptr(), B.data_ptr(), sb.data_ptr(), block, M, K, N, Y.data_ptr(),
-                                                                _stream_addr(stream)), check)
+                                                                _stream_addr(stream, dev)), check)
 
 
 def ffuse_grouped_gemm_fp8(dtype, A, sa, B, sb, offsets, Y, stream=None, check=True):
@@ -590,7 +595,7 @@ def ffuse_grouped_gemm_fp8(dtype, A, sa, B, sb, offsets, Y, stream=None, check=T
     _want(dev, "offsets", offsets, (E + 1,), torch.int32)
     _want(dev, "Y", Y, (R, N), t)
     return _rc("ffuse_grouped_gemm_fp8", (_lib or lib()).ffuse_grouped_gemm_fp8(dtype, A.data_ptr(), sa.data_ptr(), B.data_ptr(), sb.data_ptr(), block,
-                                                                                offsets.data_ptr(), R, E, K, N, Y.data_ptr(), _stream_addr(stream)), check)
+                                                                                offsets.data_ptr(), R, E, K, N, Y.data_ptr(), _stream_addr(stream, dev)), check)
 
 
 def ffuse_profile_enable(on: bool):
