@@ -19,7 +19,7 @@ namespace ffuse {
 //
 // 16384 rows in eight equal groups, and in eight uneven ones (68 row blocks for 64): gated 4096 x 11008 2249 and 2363 us
 // (1.31 and 1.25 PFLOP/s), plain 11008 x 4096 1162 and 1262, 4096 x 4096 419 and 452, the gradient of the input 428 and 454.  Bound by the bytes from
-// L2 to LDS and the power they take (the core clock is 1.5 - 1.8 GHz): copies of the last without loads in the loop ran
+// L2 to LDS and the power they take (the core clock is 1.9 - 2.1 GHz of 2.4): copies of the last without loads in the loop ran
 // 358 us instead of 449, without fragment reads 433, with every workgroup of an XCD on the same panels 416.  A larger tile would move
 // fewer bytes, but its accumulators do not fit.  512 rows of 64 experts, 1.1 GB of weights in two products: 186 us, 5.9 TB/s.
 template <typename T, bool BCOL, bool GATED, class G, class Walk>
