@@ -73,23 +73,27 @@ struct State {
 };
 State g;
 
-// the record of a per-call workspace; the caller holds the lock
+bool overlap(const Workspace& w, const void* ptr, size_t bytes) {
+    const char *a = static_cast<const char*>(ptr), *b = static_cast<const char*>(w.ptr);
+    return w.ptr && a < b + w.bytes && b < a + bytes;
+}
+// the record of a per-call workspace; the caller holds the lock.  Part of a workspace that a graph uses is one itself,
+// and the records of those are replaced last.
 Workspace& workspace_record(void* ptr, size_t bytes) {
     Workspace* oldest = &g.seen[0];
+    bool in_graph = g.reg.in_graph && overlap(g.reg, ptr, bytes);
     for (Workspace& w : g.seen) {
         if (w.ptr == ptr && w.bytes == bytes) { w.used = ++g.clock; return w; }
-        if (w.used < oldest->used) oldest = &w;
+        in_graph = in_graph || (w.in_graph && overlap(w, ptr, bytes));
+        if (w.in_graph != oldest->in_graph ? oldest->in_graph : w.used < oldest->used) oldest = &w;
     }
-    *oldest = Workspace{ptr, bytes, 0, nullptr, ++g.clock, false};
+    *oldest = Workspace{ptr, bytes, 0, nullptr, ++g.clock, in_graph};
     return *oldest;
 }
 // forget what is known about any record that overlaps [ptr, ptr + bytes): its memory is about to change hands
 void forget_overlapping(const void* ptr, size_t bytes) {
-    const char* a = static_cast<const char*>(ptr);
-    for (Workspace& w : g.seen) {
-        const char* b = static_cast<const char*>(w.ptr);
-        if (w.ptr && a < b + w.bytes && b < a + bytes) w = Workspace{};
-    }
+    for (Workspace& w : g.seen)
+        if (overlap(w, ptr, bytes)) w = Workspace{};
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -486,10 +490,8 @@ void workspace_overwritten(void* p, size_t bytes, hipStream_t st) {
     std::lock_guard<std::mutex> lock(g.mu);
     const bool recorded = stream_is_capturing(st);
     if (recorded) workspace_record(p, bytes);   // (so that a later call on it knows)
-    const char* a = static_cast<const char*>(p);
     const auto dirty = [&](Workspace& w) {
-        const char* b = static_cast<const char*>(w.ptr);
-        if (!w.ptr || a >= b + w.bytes || b >= a + bytes) return;
+        if (!overlap(w, p, bytes)) return;
         w.zero = 0;
         w.small_flags = nullptr;
         if (recorded) w.in_graph = true;

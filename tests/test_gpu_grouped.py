@@ -286,10 +286,10 @@ def test_two_streams_at_once():
 
 
 @pytest.mark.parametrize("in_graph", (False, True))
-@pytest.mark.parametrize("registered", (False, True))
-def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
+@pytest.mark.parametrize("registered,part", ((False, 1), (False, 2), (True, 1)))
+def test_a_workspace_shared_with_the_other_chains(in_graph, registered, part):
     """The chains of one expert remember what they left in a workspace; a grouped chain in between, or replayed
-    behind the library's back, makes them clear it again."""
+    behind the library's back, makes them clear it again, also where they use only a part of its memory."""
     gen, sizes = torch.Generator().manual_seed(14), [50, 78]
     X, W1, W3, W2 = _layer(gen, sizes, 136, 264, 72)
     plans = [ff.make_plan(ff.FAMILY_REDUCE, bm=128, bh=64, bn2=128, raster=1, splits=(264 + 63) // 64),       # sums that start at zero
@@ -323,7 +323,7 @@ def test_a_workspace_shared_with_the_other_chains(in_graph, registered):
                 if registered and not in_graph:
                     ff.ffuse_ffn(A, B1, None, B2, ff.ACT_RELU, Z)
                 else:
-                    ff.ffuse_ffn_ws(ff.DT_BF16, A, B1, None, B2, ff.ACT_RELU, Z, ws)
+                    ff.ffuse_ffn_ws(ff.DT_BF16, A, B1, None, B2, ff.ACT_RELU, Z, ws[: nbytes // part])
                 assert ff.ffuse_sync_status(check=False) == 0
                 u.assert_within(Z, want, err, f"chain of one expert, plan {plan.as_dict()}")
                 graph.replay() if graph else grouped()
