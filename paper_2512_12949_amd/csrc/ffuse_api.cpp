@@ -15,21 +15,11 @@
 #include "../../include/ffuse.h"
 #include "ffuse_launch.h"
 #include "ffuse_plan.h"
+#include "ffuse_workspaces.h"
 
 namespace {
 
-// What the library remembers about a caller-owned workspace between calls: how much of its start is
-// known to be zero (the reduce family keeps its sums there) and where the two-phase family last left
-// clean barrier flags.  A workspace the library has not seen (or whose size changed) counts as dirty.
-struct Workspace {
-    void* ptr = nullptr;
-    size_t bytes = 0;
-    size_t zero = 0;                  // bytes at the start known to be zero
-    uint32_t* small_flags = nullptr;  // where the two-phase family last left clean barrier flags
-    uint64_t used = 0;                // age, for replacement
-    bool in_graph = false;            // a call on this workspace was recorded into a graph: replays the library does
-                                      // not see may dirty it at any time, so nothing above is trusted any more
-};
+using ffuse::Workspace;
 
 // geometry of a 3x3 first convolution (ic == 0: the first product is a plain GEMM)
 struct ConvGeom {
@@ -38,9 +28,7 @@ struct ConvGeom {
 
 struct State {
     std::mutex mu;
-    Workspace reg;           // the workspace registered with ffuse_set_workspace
-    Workspace seen[8];       // workspaces passed per call (ffuse_ffn_ws ...), most recently used kept
-    uint64_t clock = 0;
+    ffuse::Workspaces ws;    // the caller's workspaces
     uint32_t spin_limit = 1u << 24;   // bounded waits of the two-phase barrier (ffuse_debug_barrier)
     int extra_arrivals = 0;
     int objective = FFUSE_OBJECTIVE_TIME;
@@ -72,29 +60,6 @@ struct State {
     std::map<std::array<int64_t, 7>, TableEntry> table;
 };
 State g;
-
-bool overlap(const Workspace& w, const void* ptr, size_t bytes) {
-    const char *a = static_cast<const char*>(ptr), *b = static_cast<const char*>(w.ptr);
-    return w.ptr && a < b + w.bytes && b < a + bytes;
-}
-// the record of a per-call workspace; the caller holds the lock.  Part of a workspace that a graph uses is one itself,
-// and the records of those are replaced last.
-Workspace& workspace_record(void* ptr, size_t bytes) {
-    Workspace* oldest = &g.seen[0];
-    bool in_graph = g.reg.in_graph && overlap(g.reg, ptr, bytes);
-    for (Workspace& w : g.seen) {
-        if (w.ptr == ptr && w.bytes == bytes) { w.used = ++g.clock; return w; }
-        in_graph = in_graph || (w.in_graph && overlap(w, ptr, bytes));
-        if (w.in_graph != oldest->in_graph ? oldest->in_graph : w.used < oldest->used) oldest = &w;
-    }
-    *oldest = Workspace{ptr, bytes, 0, nullptr, ++g.clock, in_graph};
-    return *oldest;
-}
-// forget what is known about any record that overlaps [ptr, ptr + bytes): its memory is about to change hands
-void forget_overlapping(const void* ptr, size_t bytes) {
-    for (Workspace& w : g.seen)
-        if (overlap(w, ptr, bytes)) w = Workspace{};
-}
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -243,7 +208,7 @@ int run_fused(int dtype, const void* X, const void* W1, const void* W3, const vo
     int rc = validate(X, W1, W3, W2, act, M, K, N1, N2, Y, elem);
     if (rc != FFUSE_OK) return rc;
     std::lock_guard<std::mutex> lock(g.mu);
-    return run_fused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);
+    return run_fused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);
 }
 
 // Weights far larger than the 256 MB memory-side cache are streamed with the non-temporal
@@ -275,13 +240,11 @@ int run_plan(const ffuse_plan_t& plan, int dtype, const void* X, const void* W1,
              const ConvGeom& conv) {
     const int gated = W3 != nullptr;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    if (stream_is_capturing(st)) w.in_graph = true;
-    if (w.in_graph) { w.zero = 0; w.small_flags = nullptr; }
-    // (and whatever this call leaves behind, a replay may find something else)
-    struct Forget {
+    g.ws.begin(w, stream_is_capturing(st));
+    struct End {
         Workspace& w;
-        ~Forget() { if (w.in_graph) { w.zero = 0; w.small_flags = nullptr; } }
-    } forget{w};
+        ~End() { g.ws.end(w); }
+    } end{w};
     ffuse::FusedArgs a{X, W1, W3, W2, nullptr, M, (int)K, (int)N1, (int)N2, act, plan.raster > 0 ? plan.raster : 1};
     if (plan.family == FFUSE_FAMILY_SCALAR) {
         Timer t(st);
@@ -300,7 +263,7 @@ int run_plan(const ffuse_plan_t& plan, int dtype, const void* X, const void* W1,
             r.stats = reinterpret_cast<uint64_t*>(w.ptr);
             g.rows_stats = r.stats;
             g.rows_wgs = (int)std::min<int64_t>((M + 63) / 64, g.cus);
-            w.zero = 0; w.small_flags = nullptr;
+            w.forget();
         }
         Timer t(st);
         const int64_t mb = (M + 63) / 64;
@@ -464,7 +427,7 @@ int run_unfused(int dtype, const void* X, const void* W1, const void* W3, const 
     int rc = validate(X, W1, W3, W2, act, M, K, N1, N2, Y, elem);
     if (rc != FFUSE_OK) return rc;
     std::lock_guard<std::mutex> lock(g.mu);
-    return run_unfused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);
+    return run_unfused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);
 }
 
 // the workspace argument of a per-call entry point: nullptr / 0 is allowed (families that need none)
@@ -488,16 +451,7 @@ int device_ready(int* cus) {
 
 void workspace_overwritten(void* p, size_t bytes, hipStream_t st) {
     std::lock_guard<std::mutex> lock(g.mu);
-    const bool recorded = stream_is_capturing(st);
-    if (recorded) workspace_record(p, bytes);   // (so that a later call on it knows)
-    const auto dirty = [&](Workspace& w) {
-        if (!overlap(w, p, bytes)) return;
-        w.zero = 0;
-        w.small_flags = nullptr;
-        if (recorded) w.in_graph = true;
-    };
-    dirty(g.reg);
-    for (Workspace& w : g.seen) dirty(w);
+    g.ws.overwritten(p, bytes, stream_is_capturing(st));
 }
 
 }  // namespace ffuse
@@ -537,7 +491,7 @@ int ffuse_ffn_ws(int dtype, const void* X, const void* W1, const void* W3, const
     if ((rc = check_ws_arg(workspace, workspace_bytes)) != FFUSE_OK) return rc;
     std::lock_guard<std::mutex> lock(g.mu);
     Workspace none;
-    return run_fused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, workspace ? workspace_record(workspace, workspace_bytes) : none, stream);
+    return run_fused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, workspace ? g.ws.named(workspace, workspace_bytes) : none, stream);
 }
 int ffuse_ffn_unfused_ws(int dtype, const void* X, const void* W1, const void* W3, const void* W2, int act, int64_t M, int64_t K,
                          int64_t N1, int64_t N2, void* Y, void* workspace, size_t workspace_bytes, void* stream) {
@@ -547,7 +501,7 @@ int ffuse_ffn_unfused_ws(int dtype, const void* X, const void* W1, const void* W
     if ((rc = check_ws_arg(workspace, workspace_bytes)) != FFUSE_OK) return rc;
     std::lock_guard<std::mutex> lock(g.mu);
     Workspace none;
-    return run_unfused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, workspace ? workspace_record(workspace, workspace_bytes) : none, stream);
+    return run_unfused_locked(dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, workspace ? g.ws.named(workspace, workspace_bytes) : none, stream);
 }
 
 }  // extern "C"
@@ -639,15 +593,14 @@ size_t ffuse_workspace_bytes(int dtype, int gated, int64_t M, int64_t K, int64_t
 int ffuse_set_workspace(void* dev_ptr, size_t bytes, void* stream) {
     std::lock_guard<std::mutex> lock(g.mu);
     if (!dev_ptr) {
-        g.reg = Workspace{};
+        g.ws.unregistered();
         g.exch_err = nullptr;
         return FFUSE_OK;
     }
     if (!aligned16(dev_ptr)) return FFUSE_ERR_ALIGN;
     if (bytes % 16) return FFUSE_ERR_SHAPE;
     if (ffuse::launch_zero(dev_ptr, bytes, reinterpret_cast<hipStream_t>(stream)) != hipSuccess) return FFUSE_ERR_LAUNCH;
-    forget_overlapping(dev_ptr, bytes);
-    g.reg = Workspace{dev_ptr, bytes, bytes, nullptr, 0, false};
+    g.ws.registered(dev_ptr, bytes);
     g.exch_err = nullptr;
     return FFUSE_OK;
 }
@@ -772,7 +725,7 @@ int ffuse_sync_status(void* stream) {
 // chain on the pixel rows; a 3x3 one runs the two-phase kernel with implicit-im2col loads.
 int run_conv_chain(int dtype, const void* X, const void* W1, const void* W2, int act, int64_t B, int64_t H, int64_t W,
                    int64_t IC, int64_t OC1, int64_t OC2, int k1, int k2, void* Y, void* stream) {
-    Workspace& ws = g.reg;
+    Workspace& ws = g.ws.reg;
     if (B < 1 || H < 1 || W < 1 || IC < 8 || H > 32768 || W > 32768) return FFUSE_ERR_SHAPE;
     if (k2 != 1 || (k1 != 1 && k1 != 3)) return FFUSE_ERR_SHAPE;
     const int64_t M = B * H * W, K = (int64_t)k1 * k1 * IC;
@@ -854,8 +807,8 @@ int ffuse_tune(int dtype, const void* X, const void* W1, const void* W3, const v
         if ((int)cands.size() >= top_k) break;
         const ffuse_plan_t& p = cand.plan;
         if (!ffuse::plan_valid(p, dtype, gated, M, K, N1, N2)) continue;
-        if (ffuse::plan_workspace_bytes(p, dtype, gated, M, K, N1, N2) > g.reg.bytes) continue;
-        last_rc = run_plan(p, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);
+        if (ffuse::plan_workspace_bytes(p, dtype, gated, M, K, N1, N2) > g.ws.reg.bytes) continue;
+        last_rc = run_plan(p, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);
         if (last_rc != FFUSE_OK) continue;
         if (hipStreamSynchronize(st) != hipSuccess) { last_rc = FFUSE_ERR_LAUNCH; stop = true; break; }
         if (g.exch_err) {
@@ -869,15 +822,15 @@ int ffuse_tune(int dtype, const void* X, const void* W1, const void* W3, const v
         // bring clocks and caches to their steady state before anything is timed, or the first
         // candidate is measured on a different chip than the last
         for (int r = 0; r < 2 * reps && last_rc == FFUSE_OK; ++r)
-            last_rc = run_plan(cands[0].plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);
+            last_rc = run_plan(cands[0].plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);
         // two timed passes, the second in reverse order (drift of the clocks cancels); a candidate's
         // time is the better of its two
         for (int pass = 0; pass < 2 && !stop; ++pass)
             for (size_t n = 0; n < cands.size(); ++n) {
                 Cand& c = cands[pass == 0 ? n : cands.size() - 1 - n];
-                last_rc = run_plan(c.plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);   // (its own warm-up: LDS size, L2 contents)
+                last_rc = run_plan(c.plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);   // (its own warm-up: LDS size, L2 contents)
                 (void)hipEventRecord(e0, st);
-                for (int r = 0; r < reps && last_rc == FFUSE_OK; ++r) last_rc = run_plan(c.plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.reg, stream);
+                for (int r = 0; r < reps && last_rc == FFUSE_OK; ++r) last_rc = run_plan(c.plan, dtype, X, W1, W3, W2, act, M, K, N1, N2, Y, g.ws.reg, stream);
                 (void)hipEventRecord(e1, st);
                 if (hipEventSynchronize(e1) != hipSuccess) { last_rc = FFUSE_ERR_LAUNCH; stop = true; break; }
                 if (last_rc != FFUSE_OK) continue;
@@ -1016,7 +969,7 @@ int ffuse_plan_lookup(int dtype, int act, int gated, int64_t M, int64_t K, int64
     if (dtype < FFUSE_DT_BF16 || dtype > FFUSE_DT_F32) return FFUSE_ERR_ACT;
     if (M < 1 || K < 8 || N1 < 8 || N2 < 8) return FFUSE_ERR_SHAPE;
     std::lock_guard<std::mutex> lock(g.mu);
-    *out = lookup_plan(dtype, act, gated ? 1 : 0, M, K, N1, N2, g.reg.ptr ? g.reg.bytes : ffuse::kAnyWorkspace);
+    *out = lookup_plan(dtype, act, gated ? 1 : 0, M, K, N1, N2, g.ws.reg.ptr ? g.ws.reg.bytes : ffuse::kAnyWorkspace);
     if (tuned_ms) {
         auto it = g.table.find(table_key(dtype, gated ? 1 : 0, K, N1, N2, ffuse::m_bin(M)));
         *tuned_ms = (it != g.table.end() && std::memcmp(&it->second.plan, out, sizeof(*out)) == 0) ? it->second.ms : 0.0;
