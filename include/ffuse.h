@@ -40,9 +40,10 @@
  *     itself must hand it over again (ffuse_set_workspace, or any other size in a _ws call).
  *   - Graph capture: a call recorded while `stream` is capturing records its own clearing of
  *     the flags or sums it needs, whatever the library believes about the workspace, and from
- *     then on every call on that workspace clears what it needs too (until the workspace is
- *     registered or named anew), so the graph may be replayed between any other calls on the
- *     same workspace (not concurrently with them).
+ *     then on every call on that workspace, or on one that overlaps it, clears what it needs too, so
+ *     the graph may be replayed between any other calls on the same workspace (not concurrently with
+ *     them).  However many workspaces graphs use, the library knows them all.  Handing memory to
+ *     ffuse_set_workspace says that no graph recorded before uses it any more.
  */
 #ifndef FFUSE_H
 #define FFUSE_H
@@ -273,7 +274,8 @@ int ffuse_grouped_gemm_fp8(int dtype, const void* A, const float* sa, const void
 /* ---- workspace.  ffuse_workspace_bytes: bytes the given problem needs (fused path when
  *      unfused == 0; with unfused != 0 the two-launch path's intermediate, partial-sum planes
  *      and flags).  ffuse_set_workspace: registers a caller-owned device buffer with the
- *      library (it is zero-filled once on `stream`); passing NULL unregisters it. --------- */
+ *      library (it is zero-filled once on `stream`); passing NULL unregisters it.  Graphs that used
+ *      this memory before must not be replayed any more. -------------------------------------- */
 size_t ffuse_workspace_bytes(int dtype, int gated, int64_t M, int64_t K, int64_t N1, int64_t N2,
                              int unfused);
 int ffuse_set_workspace(void* dev_ptr, size_t bytes, void* stream);

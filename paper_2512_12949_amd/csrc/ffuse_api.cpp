@@ -525,7 +525,7 @@ int static_workspace(Workspace** out) {
     if (!w.ptr) {
         void* ptr = nullptr;
         if (hipGetSymbolAddress(&ptr, HIP_SYMBOL(scratch)) != hipSuccess || !ptr) return FFUSE_ERR_LAUNCH;
-        w = Workspace{ptr, kStaticScratchBytes, 0, nullptr, 0, false};   // (nothing assumed about its contents)
+        w = Workspace{ptr, kStaticScratchBytes, 0, nullptr, 0};   // (nothing assumed about its contents)
     }
     *out = &w;
     return FFUSE_OK;

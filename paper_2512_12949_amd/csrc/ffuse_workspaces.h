@@ -14,8 +14,6 @@ struct Workspace {
     size_t zero = 0;                  // bytes at the start known to be zero
     uint32_t* small_flags = nullptr;  // where the two-phase family last left clean barrier flags
     uint64_t used = 0;                // age, for replacement
-    bool in_graph = false;            // a call on this workspace was recorded into a graph: replays the library does
-                                      // not see may dirty it at any time, so nothing above is trusted any more
     void forget() { zero = 0; small_flags = nullptr; }
     bool overlaps(const void* p, size_t n) const {
         const char *a = static_cast<const char*>(p), *b = static_cast<const char*>(ptr);
@@ -23,51 +21,106 @@ struct Workspace {
     }
 };
 
+// A set of addresses, as ranges in rising order that do not touch.  It never loses one: when it is full, the two ranges with the
+// least between them become one, and what lies between counts as in the set.
+class AddressRanges {
+public:
+    bool meets(const void* p, size_t bytes) const {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(p), to = from + bytes;
+        for (int i = 0; i < n_; ++i)
+            if (r_[i].from < to && from < r_[i].to) return true;
+        return false;
+    }
+    void add(const void* p, size_t bytes) {
+        Range x{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes};
+        if (bytes == 0) return;
+        int i = 0, end;
+        while (i < n_ && r_[i].to < x.from) ++i;
+        for (end = i; end < n_ && r_[end].from <= x.to; ++end) {
+            if (r_[end].from < x.from) x.from = r_[end].from;
+            if (r_[end].to > x.to) x.to = r_[end].to;
+        }
+        replace(i, end, &x, 1);
+    }
+    void remove(const void* p, size_t bytes) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(p), to = from + bytes;
+        for (int i = 0; i < n_;) {
+            const Range x = r_[i];
+            Range left[2];
+            int n = 0;
+            if (x.from < from) left[n++] = Range{x.from, x.to < from ? x.to : from};
+            if (x.to > to) left[n++] = Range{x.from > to ? x.from : to, x.to};
+            if (n == 2 && n_ == kMost) return;   // (no room for both ends: all of it stays)
+            replace(i, i + 1, left, n);
+            i += n;
+        }
+    }
+
+private:
+    struct Range { uintptr_t from, to; };
+    static constexpr int kMost = 256;
+    Range r_[kMost + 1];
+    int n_ = 0;
+
+    // ranges i .. end - 1 by `count` others
+    void replace(int i, int end, const Range* with, int count) {
+        const int move = count - (end - i);
+        if (move < 0) for (int j = end; j < n_; ++j) r_[j + move] = r_[j];
+        else for (int j = n_ - 1; j >= end; --j) r_[j + move] = r_[j];
+        for (int j = 0; j < count; ++j) r_[i + j] = with[j];
+        n_ += move;
+        if (n_ <= kMost) return;
+        int least = 1;
+        for (int j = 2; j < n_; ++j)
+            if (r_[j].from - r_[j - 1].to < r_[least].from - r_[least - 1].to) least = j;
+        r_[least - 1].to = r_[least].to;
+        for (int j = least + 1; j < n_; ++j) r_[j - 1] = r_[j];
+        --n_;
+    }
+};
+
 struct Workspaces {
     Workspace reg;           // the workspace registered with ffuse_set_workspace
     Workspace seen[8];       // workspaces passed per call (ffuse_ffn_ws ...), most recently used kept
     uint64_t clock = 0;
+    AddressRanges recorded;  // workspaces of calls that were recorded into graphs: replays the library does not see may
+                             // dirty them at any time, so nothing is remembered of a workspace that one of them overlaps
 
-    // The record of a per-call workspace.  Part of a workspace that a graph uses is one itself, and the records of those are
-    // replaced last.
+    // the record of a per-call workspace
     Workspace& named(void* ptr, size_t bytes) {
         Workspace* oldest = &seen[0];
-        bool in_graph = reg.in_graph && reg.overlaps(ptr, bytes);
         for (Workspace& w : seen) {
             if (w.ptr == ptr && w.bytes == bytes) { w.used = ++clock; return w; }
-            in_graph = in_graph || (w.in_graph && w.overlaps(ptr, bytes));
-            if (w.in_graph != oldest->in_graph ? oldest->in_graph : w.used < oldest->used) oldest = &w;
+            if (w.used < oldest->used) oldest = &w;
         }
-        *oldest = Workspace{ptr, bytes, 0, nullptr, ++clock, in_graph};
+        *oldest = Workspace{ptr, bytes, 0, nullptr, ++clock};
         return *oldest;
     }
-    // [ptr, ptr + bytes), all zeros, becomes the registered workspace: its memory may have been in other hands in between
+    // [ptr, ptr + bytes), all zeros, becomes the registered workspace: its memory may have been in other hands in between, and graphs
+    // that used it are no more
     void registered(void* ptr, size_t bytes) {
         for (Workspace& w : seen)
             if (w.overlaps(ptr, bytes)) w = Workspace{};
-        reg = Workspace{ptr, bytes, bytes, nullptr, 0, false};
+        recorded.remove(ptr, bytes);
+        reg = Workspace{ptr, bytes, bytes, nullptr, 0};
     }
     void unregistered() { reg = Workspace{}; }
 
     // A call that runs in `w`, recorded into a graph or not, from before its first launch to after its last.  (Whatever a call on
     // a workspace that a graph uses leaves behind, a replay may find something else.)
-    void begin(Workspace& w, bool recorded) {
-        if (recorded) w.in_graph = true;
+    void begin(Workspace& w, bool into_graph) {
+        if (into_graph) recorded.add(w.ptr, w.bytes);
         end(w);
     }
     void end(Workspace& w) {
-        if (w.in_graph) w.forget();
+        if (recorded.meets(w.ptr, w.bytes)) w.forget();
     }
     // a call of another kind, recorded into a graph or not, writes into [ptr, ptr + bytes)
-    void overwritten(void* ptr, size_t bytes, bool recorded) {
-        if (recorded) named(ptr, bytes);   // (so that a later call on it knows)
-        const auto dirty = [&](Workspace& w) {
-            if (!w.overlaps(ptr, bytes)) return;
-            w.forget();
-            if (recorded) w.in_graph = true;
-        };
-        dirty(reg);
-        for (Workspace& w : seen) dirty(w);
+    void overwritten(void* ptr, size_t bytes, bool into_graph) {
+        if (into_graph) recorded.add(ptr, bytes);
+        if (reg.overlaps(ptr, bytes)) reg.forget();
+        for (Workspace& w : seen)
+            if (w.overlaps(ptr, bytes)) w.forget();
     }
 };
 
