@@ -37,7 +37,9 @@
  *     streams) need different workspaces: give each stream its own through the _ws calls.
  *     Between calls the library remembers, per workspace address, what it left there (which
  *     part is zero, where clean barrier flags lie); a caller that writes into a workspace
- *     itself must hand it over again (ffuse_set_workspace, or any other size in a _ws call).
+ *     itself must hand it over again (ffuse_set_workspace, or any size but the last one in a _ws call).
+ *     Workspaces may share memory, as long as their calls do not overlap in time: a call on one makes
+ *     the next call on the other clear what it needs.
  *   - Graph capture: a call recorded while `stream` is capturing records its own clearing of
  *     the flags or sums it needs, whatever the library believes about the workspace, and from
  *     then on every call on that workspace, or on one that overlaps it, clears what it needs too, so
@@ -169,7 +171,7 @@ int ffuse_ffn_f32(const void* X, const void* W1, const void* W3, const void* W2,
  * device pointer, 16-byte aligned, of `workspace_bytes` bytes (a multiple of 16); NULL / 0 is
  * accepted and runs the plans that need none (FFUSE_ERR_WORKSPACE otherwise).  Nothing about
  * the workspace has to be prepared by the caller: a workspace the library has not seen before
- * (or sees with another size) is treated as dirty, and the call clears what it needs on `stream`.
+ * (or sees with another size than the last time) is treated as dirty, and the call clears what it needs on `stream`.
  * Two streams with two workspaces may overlap in time. */
 int ffuse_ffn_ws(int dtype, const void* X, const void* W1, const void* W3, const void* W2, int act,
                  int64_t M, int64_t K, int64_t N1, int64_t N2, void* Y, void* workspace,

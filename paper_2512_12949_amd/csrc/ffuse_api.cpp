@@ -126,6 +126,14 @@ bool stream_is_capturing(hipStream_t st) {
     return hipStreamIsCapturing(st, &cs) == hipSuccess && cs != hipStreamCaptureStatusNone;
 }
 
+// a call that runs in `w`, for as long as it launches
+struct WorkspaceUse {
+    Workspace& w;
+    WorkspaceUse(Workspace& ws, hipStream_t st) : w(ws) { g.ws.begin(w, stream_is_capturing(st)); }
+    ~WorkspaceUse() { g.ws.end(w); }
+    WorkspaceUse(const WorkspaceUse&) = delete;
+};
+
 struct Timer {  // brackets the dominant kernel with events when profiling is on
     hipStream_t st;
     hipEvent_t a = nullptr, b = nullptr;
@@ -240,11 +248,7 @@ int run_plan(const ffuse_plan_t& plan, int dtype, const void* X, const void* W1,
              const ConvGeom& conv) {
     const int gated = W3 != nullptr;
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    g.ws.begin(w, stream_is_capturing(st));
-    struct End {
-        Workspace& w;
-        ~End() { g.ws.end(w); }
-    } end{w};
+    const WorkspaceUse use(w, st);
     ffuse::FusedArgs a{X, W1, W3, W2, nullptr, M, (int)K, (int)N1, (int)N2, act, plan.raster > 0 ? plan.raster : 1};
     if (plan.family == FFUSE_FAMILY_SCALAR) {
         Timer t(st);
@@ -409,8 +413,8 @@ int run_unfused_locked(int dtype, const void* X, const void* W1, const void* W3,
     }
     const size_t need = (size_t)elem * (size_t)M * (size_t)N1;
     if (!w.ptr || w.bytes < need) return FFUSE_ERR_WORKSPACE;
-    w.zero = 0;      // H overwrites whatever the fused path kept at zero
-    w.small_flags = nullptr;
+    const WorkspaceUse use(w, st);
+    w.forget();      // H overwrites whatever the fused path kept at zero
     g.exch_err = nullptr;
     ffuse::GemmArgs g0{X, W1, W3, w.ptr, M, (int)K, (int)N1, act};
     ffuse::GemmArgs g1{w.ptr, W2, nullptr, Y, M, (int)N1, (int)N2, FFUSE_ACT_IDENTITY};
@@ -599,8 +603,9 @@ int ffuse_set_workspace(void* dev_ptr, size_t bytes, void* stream) {
     }
     if (!aligned16(dev_ptr)) return FFUSE_ERR_ALIGN;
     if (bytes % 16) return FFUSE_ERR_SHAPE;
-    if (ffuse::launch_zero(dev_ptr, bytes, reinterpret_cast<hipStream_t>(stream)) != hipSuccess) return FFUSE_ERR_LAUNCH;
-    g.ws.registered(dev_ptr, bytes);
+    hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    if (ffuse::launch_zero(dev_ptr, bytes, st) != hipSuccess) return FFUSE_ERR_LAUNCH;
+    g.ws.registered(dev_ptr, bytes, stream_is_capturing(st));
     g.exch_err = nullptr;
     return FFUSE_OK;
 }

@@ -96,31 +96,33 @@ struct Workspaces {
         *oldest = Workspace{ptr, bytes, 0, nullptr, ++clock};
         return *oldest;
     }
-    // [ptr, ptr + bytes), all zeros, becomes the registered workspace: its memory may have been in other hands in between, and graphs
-    // that used it are no more
-    void registered(void* ptr, size_t bytes) {
+    // [ptr, ptr + bytes) becomes the registered workspace: its memory may have been in other hands in between, and graphs that used
+    // it are no more.  It is cleared now, or, into_graph, whenever the graph is replayed.
+    void registered(void* ptr, size_t bytes, bool into_graph) {
         for (Workspace& w : seen)
             if (w.overlaps(ptr, bytes)) w = Workspace{};
         recorded.remove(ptr, bytes);
-        reg = Workspace{ptr, bytes, bytes, nullptr, 0};
+        if (into_graph) recorded.add(ptr, bytes);
+        reg = Workspace{ptr, bytes, into_graph ? 0 : bytes, nullptr, 0};
     }
     void unregistered() { reg = Workspace{}; }
 
-    // A call that runs in `w`, recorded into a graph or not, from before its first launch to after its last.  (Whatever a call on
-    // a workspace that a graph uses leaves behind, a replay may find something else.)
+    // A call that runs in `w`, recorded into a graph or not, from before its first launch to after its last.  What is known of
+    // other records that share memory with it no longer holds.  (Whatever a call on a workspace that a graph uses leaves behind, a
+    // replay may find something else.)
     void begin(Workspace& w, bool into_graph) {
-        if (into_graph) recorded.add(w.ptr, w.bytes);
+        overwritten(w.ptr, w.bytes, into_graph, &w);
         end(w);
     }
     void end(Workspace& w) {
         if (recorded.meets(w.ptr, w.bytes)) w.forget();
     }
-    // a call of another kind, recorded into a graph or not, writes into [ptr, ptr + bytes)
-    void overwritten(void* ptr, size_t bytes, bool into_graph) {
+    // A call, recorded into a graph or not, writes into [ptr, ptr + bytes); `own`: the record, if any, that it keeps itself.
+    void overwritten(void* ptr, size_t bytes, bool into_graph, const Workspace* own = nullptr) {
         if (into_graph) recorded.add(ptr, bytes);
-        if (reg.overlaps(ptr, bytes)) reg.forget();
+        if (&reg != own && reg.overlaps(ptr, bytes)) reg.forget();
         for (Workspace& w : seen)
-            if (w.overlaps(ptr, bytes)) w.forget();
+            if (&w != own && w.overlaps(ptr, bytes)) w.forget();
     }
 };
 

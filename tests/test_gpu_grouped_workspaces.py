@@ -96,3 +96,46 @@ def test_a_registered_workspace_that_a_graph_uses():
             w.chain(plan, ws, f"no longer registered, step {step}")
             graph.replay()
             torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("whole", ("eager", "recorded", "registered", "grouped"))
+def test_the_whole_of_a_workspace_after_its_half(whole):
+    """What is remembered of the half does not outlive a call on the whole."""
+    w, ws = _Work(32), _workspace()
+    half = ws[: 1 << 19]
+    for first, other in ((SUMS, FLAGS), (FLAGS, SUMS)):
+        w.chain(first, half, "half")
+        w.chain(first, half, "half, again")
+        use = {"grouped": lambda: w.grouped(ws), "recorded": lambda: w.chain(other, ws, "whole")}.get(whole, lambda: w.chain(other, ws, "whole"))
+        if whole == "recorded":
+            Z = torch.empty((100, N2), dtype=BF16, device="cuda")
+            ff.ffuse_force_plan(other)
+            try:
+                use = w.recorded(lambda: ff.ffuse_ffn_ws(ff.DT_BF16, w.A, w.B1, None, w.B2, ff.ACT_RELU, Z, ws)).replay
+            finally:
+                ff.ffuse_force_plan(None)
+        elif whole == "registered":
+            gu.Workspace.buf = None
+            ff.ffuse_set_workspace(ws)
+            w.chain(first, half, "half of the registered one")
+            use = lambda: w.chain(other, None, "registered")  # noqa: E731
+        for step in range(3):
+            use()
+            torch.cuda.synchronize()
+            w.chain(first, half, f"half after the whole, {whole}, step {step}")
+        if whole == "registered":
+            ff.ffuse_set_workspace(None)
+
+
+def test_the_fp32_path_of_two_launches_in_a_graph():
+    """Its intermediate, written by replays, over another chain's sums."""
+    w, ws = _Work(33), _workspace()
+    A, B1, B2 = (torch.ones(s, device="cuda") for s in ((100, K), (K, N1), (N1, N2)))
+    Z = torch.empty((100, N2), device="cuda")
+    graph = w.recorded(lambda: ff.ffuse_ffn_unfused_ws(ff.DT_F32, A, B1, None, B2, ff.ACT_RELU, Z, ws))
+    for plan in (SUMS, FLAGS):
+        for step in range(3):
+            w.chain(plan, ws, f"step {step}")
+            graph.replay()
+            torch.cuda.synchronize()
+            assert bool((Z == K * N1).all())

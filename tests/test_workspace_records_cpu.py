@@ -38,7 +38,7 @@ int flags(char* p, size_t bytes, size_t at, int recorded) {
     return clears;
 }
 void overwritten(char* p, size_t bytes, int recorded) { ws.overwritten(p, bytes, recorded); }
-void registered(char* p, size_t bytes) { ws.registered(p, bytes); }
+void registered(char* p, size_t bytes, int recorded) { ws.registered(p, bytes, recorded); }
 void unregistered() { ws.unregistered(); }
 static ffuse::AddressRanges ranges;
 void ranges_reset() { ranges = ffuse::AddressRanges(); }
@@ -58,7 +58,7 @@ def lib(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-I", CSRC, str(d / "driver.cpp"), "-o", str(d / "driver.so")], check=True)
     L = ctypes.CDLL(str(d / "driver.so"))
     n, p, i = ctypes.c_size_t, ctypes.c_void_p, ctypes.c_int
-    for name, args in (("reset", []), ("sums", [p, n, n, i]), ("flags", [p, n, n, i]), ("overwritten", [p, n, i]), ("registered", [p, n]), ("unregistered", []),
+    for name, args in (("reset", []), ("sums", [p, n, n, i]), ("flags", [p, n, n, i]), ("overwritten", [p, n, i]), ("registered", [p, n, i]), ("unregistered", []),
                        ("ranges_reset", []), ("ranges_add", [p, n]), ("ranges_remove", [p, n]), ("ranges_meet", [p, n])):
         getattr(L, name).argtypes = args
     L.reset()
@@ -131,7 +131,7 @@ def test_registering_is_the_end_of_graphs(lib):
     """ffuse_set_workspace hands memory over: it is cleared there, and remembered again, as far as the registered workspace goes."""
     lib.reset()
     lib.overwritten(_place(0), 4 * SIZE, 1)
-    lib.registered(_place(1), SIZE)
+    lib.registered(_place(1), SIZE, 0)
     assert [lib.sums(None, 0, 512, 0) for _ in range(3)] == [0, 0, 0]
     assert [lib.sums(_place(2), SIZE, 512, 0) for _ in range(3)] == [1, 1, 1]
     lib.unregistered()
@@ -142,9 +142,105 @@ def test_registering_is_the_end_of_graphs(lib):
 def test_a_recorded_registered_workspace_stays_one(lib):
     """Whoever names its memory afterwards, and after it is registered no more."""
     lib.reset()
-    lib.registered(_place(0), SIZE)
+    lib.registered(_place(0), SIZE, 0)
     lib.sums(None, 0, 512, 1)
     assert [lib.sums(None, 0, 512, 0) for _ in range(3)] == [1, 1, 1]
     assert [lib.sums(_place(0), SIZE // 2, 512, 0) for _ in range(3)] == [1, 1, 1]
     lib.unregistered()
     assert [lib.sums(_place(0), SIZE, 512, 0) for _ in range(3)] == [1, 1, 1]
+
+
+class _Memory:
+    """What really lies in memory, a letter a word of 64 bytes, beside what the records say.  A call that leaves out its clearing where
+    it should not have fails here."""
+    WORDS, WORD = 64, 64
+
+    def __init__(self, lib):
+        lib.reset()
+        self.lib, self.words, self.reg, self.graphs = lib, ["?"] * self.WORDS, None, []
+
+    def call(self, kind, space, need, into_graph=False):
+        """space: (first word, words), or None for the registered one; need: words of sums, or of data before the flags."""
+        first, n = space or self.reg
+        args = (BASE + first * self.WORD, n * self.WORD) if space else (None, 0)
+        if kind == "grouped":
+            self.lib.overwritten(BASE + first * self.WORD, n * self.WORD, into_graph)
+            todo = [("H", first, need)]
+        else:
+            clears = getattr(self.lib, kind)(*args, need * self.WORD, into_graph)
+            if kind == "sums":
+                todo = ([("0", first, need)] if clears else []) + [("0?", first, need)]
+            else:      # (clean flags are zeros; what is zero may as well be flags)
+                todo = ([("0", first + need, 1)] if clears else []) + [("0?", first + need, 1), ("H", first, need)]
+        if into_graph:
+            assert kind == "grouped" or clears
+            self.graphs.append(todo)
+        else:
+            self.run(todo)
+
+    def run(self, todo):
+        for what, first, n in todo:
+            if what == "0?":
+                assert self.words[first:first + n] == ["0"] * n, f"{n} words from {first} on are not zero: {self.words}"
+            else:
+                self.words[first:first + n] = [what] * n
+
+    def register(self, first, n):
+        self.lib.registered(BASE + first * self.WORD, n * self.WORD, 0)
+        self.words[first:first + n] = ["0"] * n
+        self.reg, self.graphs = (first, n), [g for g in self.graphs if all(a + k <= first or first + n <= a for _, a, k in g)]
+
+
+@pytest.mark.parametrize("kind", ("grouped", "sums", "flags"))
+@pytest.mark.parametrize("into_graph", (False, True))
+def test_a_call_on_the_whole_of_a_workspace_is_one_on_its_half(lib, kind, into_graph):
+    """The half's record, and the registered workspace's, are there before the whole is used."""
+    m = _Memory(lib)
+    m.register(40, 8)
+    for _ in range(2):
+        m.call("sums", (0, 8), 4)
+        m.call("sums", None, 4)
+    m.call(kind, (0, 16), 12, into_graph)
+    m.call(kind, (32, 24), 20, into_graph)
+    for g in m.graphs:
+        m.run(g)
+    m.call("sums", (0, 8), 4)
+    m.call("sums", None, 4)
+    for g in m.graphs:
+        m.run(g)
+    m.call("sums", (0, 8), 4)
+    m.call("sums", None, 4)
+
+
+def test_another_size_hands_a_workspace_over(lib):
+    """Also a size that was named before."""
+    m = _Memory(lib)
+    for _ in range(4):
+        for n in (16, 12):
+            m.words[0:16] = ["the caller's"] * 16
+            m.call("sums", (0, n), 8)
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_calls_and_replays_in_any_order(lib, seed):
+    """Workspaces that overlap or not, used by turns, recorded, replayed and registered: whatever is left out was not needed."""
+    rng, m = random.Random(seed), _Memory(lib)
+    spaces = [(first, n) for first, n in ((rng.randrange(0, 48), rng.choice((4, 6, 8, 12, 16))) for _ in range(rng.choice((2, 4, 14))))]
+    m.register(*rng.choice(spaces))
+    for _ in range(400):
+        what = rng.random()
+        if what < 0.06 and m.graphs:
+            m.run(rng.choice(m.graphs))
+        elif what < 0.08:
+            m.register(*rng.choice(spaces))
+        else:
+            space = None if rng.random() < 0.2 else rng.choice(spaces)
+            m.call(rng.choice(("sums", "sums", "flags", "grouped")), space if space or what < 0.5 else m.reg, rng.randrange(1, (space or m.reg)[1]),
+                   into_graph=seed % 2 == 1 and rng.random() < 0.02)
+
+
+def test_registered_while_recording(lib):
+    """Its clearing is part of the graph: nothing has been cleared yet, and a replay clears sums at any time."""
+    lib.reset()
+    lib.registered(_place(0), SIZE, 1)
+    assert [lib.sums(None, 0, 512, 0) for _ in range(3)] == [1, 1, 1]
