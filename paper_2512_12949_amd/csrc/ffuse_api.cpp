@@ -453,10 +453,11 @@ int device_ready(int* cus) {
     return rc;
 }
 
-void workspace_overwritten(void* p, size_t bytes, hipStream_t st) {
-    std::lock_guard<std::mutex> lock(g.mu);
+WorkspaceWrite::WorkspaceWrite(void* p, size_t bytes, hipStream_t st) {
+    g.mu.lock();
     g.ws.overwritten(p, bytes, stream_is_capturing(st));
 }
+WorkspaceWrite::~WorkspaceWrite() { g.mu.unlock(); }
 
 }  // namespace ffuse
 

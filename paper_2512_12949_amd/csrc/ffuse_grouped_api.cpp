@@ -110,7 +110,7 @@ int ffuse_grouped_ffn(int dtype, const void* X, const void* W1, const void* W3, 
     if (!workspace || workspace_bytes < (size_t)R * (size_t)N1 * 2) return FFUSE_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return FFUSE_ERR_ALIGN;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    ffuse::workspace_overwritten(workspace, workspace_bytes, st);
+    const ffuse::WorkspaceWrite write(workspace, workspace_bytes, st);
     rc = status(ffuse::launch_grouped_forward(dtype, grouped_args(X, W1, W3, offsets, workspace, R, E, K, N1, act), cus, st));
     if (rc != FFUSE_OK) return rc;
     return status(ffuse::launch_grouped_forward(dtype, grouped_args(workspace, W2, nullptr, offsets, Y, R, E, N1, N2, FFUSE_ACT_IDENTITY), cus, st));

@@ -184,9 +184,15 @@ hipError_t launch_zero(void* p, size_t bytes, hipStream_t st);
 
 // FFUSE_OK and the number of compute units where the current device is one the kernels are for, or a status
 int device_ready(int* cus);
-// A call of another kind is about to write into [p, p + bytes) on `st`: what the library remembers about workspaces
-// there no longer holds, nor will it between calls once the writing is part of a graph.
-void workspace_overwritten(void* p, size_t bytes, hipStream_t st);
+// A call of another kind writes into [p, p + bytes) on `st`: what the library remembers about workspaces there no longer
+// holds, nor will it between calls once the writing is part of a graph.  Lives until the call has launched all it launches, and
+// no other call that uses a workspace launches in between.
+class WorkspaceWrite {
+public:
+    WorkspaceWrite(void* p, size_t bytes, hipStream_t st);
+    ~WorkspaceWrite();
+    WorkspaceWrite(const WorkspaceWrite&) = delete;
+};
 
 // fp32 debug path
 hipError_t launch_fused_f32(const FusedArgs& a, float* Y, hipStream_t st);
