@@ -325,7 +325,8 @@ int ffuse_last_plan(ffuse_plan_t* out);
  * exchange-family launch ran to completion: FFUSE_OK, or FFUSE_ERR_TIMEOUT if a workgroup's
  * bounded wait for a peer expired, or FFUSE_ERR_PLACEMENT if the exchange family's XCD-local
  * protocol found a workgroup on the wrong XCD (the output of that call is then undefined;
- * force coherent = 1).  Other families always report OK. */
+ * force coherent = 1).  Other families always report OK, and so does a launch whose workspace another kind
+ * of call or a replayed graph has written into since: its verdict lay there. */
 int ffuse_sync_status(void* stream);
 
 /* ---- plan table and on-device tuning (Sec. 4.3: the dynamic dimension M is covered by plans

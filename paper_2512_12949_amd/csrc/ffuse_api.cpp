@@ -455,7 +455,10 @@ int device_ready(int* cus) {
 
 WorkspaceWrite::WorkspaceWrite(void* p, size_t bytes, hipStream_t st) {
     g.mu.lock();
-    g.ws.overwritten(p, bytes, stream_is_capturing(st));
+    const bool recorded = stream_is_capturing(st);
+    g.ws.overwritten(p, bytes, recorded);
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p), word = reinterpret_cast<uintptr_t>(g.exch_err);
+    if (!recorded && word >= from && word < from + bytes) g.exch_err = nullptr;   // (the last launch's verdict is gone)
 }
 WorkspaceWrite::~WorkspaceWrite() { g.mu.unlock(); }
 
@@ -707,6 +710,7 @@ int ffuse_sync_status(void* stream) {
     if (!g.exch_err) return FFUSE_OK;
     uint32_t word = 0;
     if (hipMemcpy(&word, g.exch_err, sizeof(word), hipMemcpyDeviceToHost) != hipSuccess) return FFUSE_ERR_LAUNCH;
+    if (word > 3u) word = 0;   // (no verdict: a replayed graph has had the workspace since)
     if (g.log && g.exch_stats) {
         std::vector<uint64_t> h(4 * (size_t)g.exch_wgs);
         if (hipMemcpy(h.data(), g.exch_stats, h.size() * 8, hipMemcpyDeviceToHost) == hipSuccess) {

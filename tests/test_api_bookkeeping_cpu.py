@@ -31,7 +31,7 @@ X, W, Y, OFF = _Space(), _Space(), _Space(), _Space()
 
 
 def _grouped(lib, ws):
-    return lib.ffuse_grouped_ffn(0, X.at, W.at, None, W.at, OFF.at, ff.ACT_SILU, M, 2, K, N1, N2, Y.at, ws.at, ws.bytes, None)
+    return lib.ffuse_grouped_ffn(0, X.at, W.at, None, W.at, OFF.at, ff.ACT_SILU, 2 * M, 2, K, N1, N2, Y.at, ws.at, ws.bytes, None)
 
 
 def _chain(lib, ws, plan):
@@ -54,3 +54,33 @@ def test_no_call_gets_between_the_bookkeeping_of_a_chain_by_expert_and_its_launc
     assert _chain(lib, ws, SUMS) == 0
     first.join()
     assert api_stub.log(lib) == ["grouped", "held", "grouped", "zero", "reduce", "finalize"]
+
+
+FLAGS = ff.make_plan(ff.FAMILY_TWOPHASE, bm=128, splits=1, raster=2)
+
+
+@pytest.mark.parametrize("replayed", (False, True))
+def test_no_status_is_read_from_what_a_chain_by_expert_wrote(lib, replayed):
+    """The verdict of a two-phase launch lies in its workspace; an intermediate written over it, by a call or by a replay behind the
+    library's back, says nothing about that launch."""
+    ws = _Space()
+    lib.stub_reset(b"", 0)
+    assert _chain(lib, ws, FLAGS) == 0 and lib.ffuse_sync_status(None) == 0
+    if replayed:
+        ctypes.memset(ws.at, 0x3f, 2 * M * N1 * 2)
+    else:
+        assert _grouped(lib, ws) == 0
+    assert lib.ffuse_sync_status(None) == 0
+    assert _chain(lib, ws, FLAGS) == 0 and _chain(lib, ws, FLAGS) == 0 and lib.ffuse_sync_status(None) == 0
+
+
+@pytest.mark.parametrize("word,status", ((0, 0), (1, -9), (2, -10), (3, -10)))
+def test_a_verdict_is_reported(lib, word, status):
+    ws = _Space()
+    lib.stub_reset(b"", 0)
+    assert _chain(lib, ws, FLAGS) == 0
+    flags = ws.at + (2 * M * N1 + 255) // 256 * 256
+    ctypes.c_uint32.from_address(flags + 12).value = word
+    assert lib.ffuse_sync_status(None) == status
+    other = _Space()      # (a chain by expert elsewhere does not hide it)
+    assert _grouped(lib, other) == 0 and lib.ffuse_sync_status(None) == status

@@ -139,3 +139,16 @@ def test_the_fp32_path_of_two_launches_in_a_graph():
             graph.replay()
             torch.cuda.synchronize()
             assert bool((Z == K * N1).all())
+
+
+def test_a_status_is_no_part_of_an_intermediate():
+    """ffuse_sync_status after a chain by expert, and after a replay of one, in the workspace of a two-phase call."""
+    w, ws = _Work(34), _workspace()
+    graph = w.recorded(lambda: w.grouped(ws))
+    w.chain(FLAGS, ws, "before")
+    w.grouped(ws)
+    assert ff.ffuse_sync_status(check=False) == 0
+    w.chain(FLAGS, ws, "between")
+    graph.replay()
+    torch.cuda.synchronize()
+    assert ff.ffuse_sync_status(check=False) == 0
