@@ -59,7 +59,7 @@ extern "C" {
 
 typedef enum {
     FFUSE_ACT_IDENTITY = 0,  /* x                                                         */
-    FFUSE_ACT_RELU = 1,      /* max(x, 0)                                                 */
+    FFUSE_ACT_RELU = 1,      /* max(x, 0); of NaN: 0 in the chains of one expert, NaN in the products by expert */
     FFUSE_ACT_GELU_TANH = 2, /* 0.5 x (1 + tanh( sqrt(2/pi) (x + 0.044715 x^3) ))         */
     FFUSE_ACT_SILU = 3       /* x / (1 + exp(-x))   (the activation Sec. 4.1 names)       */
 } ffuse_act_t;

@@ -123,6 +123,12 @@ template <typename T> __device__ __forceinline__ f32x4 mma16(typename Mma<T>::ve
 template <> __device__ __forceinline__ f32x4 mma16<__bf16>(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 template <> __device__ __forceinline__ f32x4 mma16<_Float16>(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
+// The activations of the products by expert: as everywhere, but ReLU leaves NaN as it is, where the chains of one expert make it
+// zero.  v_maximum3_f32, one instruction as there.
+template <int ACT> __device__ __forceinline__ float activate_keep_nan(float x) {
+    return ACT == ACT_RELU ? __builtin_elementwise_maximum(x, 0.0f) : activate<ACT>(x);
+}
+
 // A tile of accumulators of 16 x 16 products (computed transposed: a lane has four neighbouring columns of a row) on its way out:
 // 16 rows of a wave's COLS columns at a time through LDS of the wave's own, so that a row's part is stored in one piece.
 // Every wave issues MT * STORES stores, those of rows and columns that do not exist out of range.
@@ -259,7 +265,7 @@ template <typename T, bool ACOL, bool BCOL, bool GATED, int BM_, int BN_, int WM
         for (int e = 0; e < WNR / ECOL; ++e)
             Store::store(smem + EPI + wave * Store::LDS_BYTES, C, ldc, wave % WM * WMR, wave / WM * WNR + e * ECOL, BM, have_m, have_n, [&](int h, int mt, int r) {
                 const int ht = e * (ECOL / 16) + h;
-                const float v = activate<ACT>(acc[0][ht][mt][r]);
+                const float v = activate_keep_nan<ACT>(acc[0][ht][mt][r]);
                 return GATED ? v * acc[G - 1][ht][mt][r] : v;
             });
     }
