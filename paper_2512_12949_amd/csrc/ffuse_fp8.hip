@@ -557,6 +557,7 @@ template <typename T, int BLOCK> static hipError_t tiles(const Fp8Args& a, int c
     typedef Fp8Gemm<T, 64, 64, 2, 2, 4, BLOCK> S64;
     static_assert(G256::LDS_BYTES <= kLdsBesideGroups && G128::LDS_BYTES <= kLdsBesideGroups && G64::LDS_BYTES <= kLdsBesideGroups &&
                   G32::LDS_BYTES <= kLdsBesideGroups && S64::LDS_BYTES <= kLdsBesideGroups, "only W128 leaves less than the largest tables");
+    static_assert(most_groups(S64::LDS_BYTES, kFp8[5].per_cu) >= kMaxGroups, "two workgroups a CU");
     const int i = pick_tile(kFp8, a.R, a.E, a.N, a.K, cus, a.E > kFp8Groups ? 1 : -1);
     switch (i) {
         case 0: return product<G256, G128>(a, kFp8[i], cus, st);

@@ -133,7 +133,12 @@ template <typename T> static hipError_t gated(const GroupedArgs& a, int cus, hip
     typedef PairGemm<T, false, true, true, 64, 128, 2, 4, 3> G64;
     typedef PairGemm<T, false, true, true, 32, 128, 1, 4, 3> G32;
     typedef PairGemm<T, false, true, true, 64, 64, 2, 2, 3> S64;
-    const int i = pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus);
+    // The last tile's tables leave room for one workgroup a CU where there are more than 512 groups: it is only taken where one is all
+    // that a CU gets.  us, as for two a CU -> this: 125 rows in 813 groups, 416 x 176, 29.2 -> 17.6; 34218 in 1018, 560 x 64, 63.2 -> 48.8.
+    // (Never above 512 groups: 65 rows in 839, 1776 x 64, 24.8 -> 26.8.)
+    const bool alone = a.E > most_groups(S64::LDS_BYTES, kGated[4].per_cu);
+    const bool full = most_row_blocks(a.R, a.E, S64::BM) * ((a.N + S64::BN - 1) / S64::BN) > cus;
+    const int i = pick_tile(kGated, a.R, a.E, a.N, 2 * (int64_t)a.K, cus, alone && full ? 4 : -1);
     switch (i) {
         case 0: return rows<T, true, true, G256, Q256>(a, kGated[i], cus, st);
         case 1: return rows<T, true, true, G128, G64>(a, kGated[i], cus, st);
@@ -150,6 +155,7 @@ template <typename T, bool BCOL> static hipError_t plain(const GroupedArgs& a, i
     typedef PairGemm<T, false, BCOL, false, 64, 128, 2, 4, 4> G64;
     typedef PairGemm<T, false, BCOL, false, 32, 128, 1, 4, 4> G32;
     typedef PairGemm<T, false, BCOL, false, 64, 64, 2, 2, 4> S64;
+    static_assert(most_groups(S64::LDS_BYTES, kPlain[6].per_cu) >= kMaxGroups && kInput[6].per_cu == kPlain[6].per_cu, "two workgroups a CU");
     const int i = BCOL ? pick_tile(kPlain, a.R, a.E, a.N, 2 * (int64_t)a.K, cus) : pick_tile(kInput, a.R, a.E, a.K, 2 * (int64_t)a.N, cus);
     const Tile& t = BCOL ? kPlain[i] : kInput[i];
     switch (i) {

@@ -16,6 +16,8 @@ static constexpr int kGroupBand = 8;      // row blocks that share their column 
 __host__ __device__ constexpr int group_table_bytes(int E) { return 8 * E; }
 // LDS that the kernels' own arrays may take beside the largest tables (160 KB in all)
 static constexpr int kLdsBesideGroups = 160 * 1024 - group_table_bytes(kMaxGroups);
+// groups whose tables leave a CU room for `per_cu` workgroups with `lds` bytes of arrays of their own
+constexpr int most_groups(int lds, int per_cu) { return (160 * 1024 / per_cu - lds) / group_table_bytes(1); }
 
 struct Groups {
     int* start;   // [E]: the clamped boundaries
