@@ -229,8 +229,10 @@ int ffuse_conv_chain_f16(const void* X, const void* W1, const void* W2, int act,
  *      which expert is unspecified, every access stays inside the tensors).  Groups may be empty; rows before offsets[0]
  *      and from offsets[E] on belong to no group, and what the output holds there is left as it is.
  *      dtype: FFUSE_DT_BF16 or FFUSE_DT_F16; fp32 sums, rounded once.  R >= 0 (R = 0: nothing to do, A and C may be
- *      NULL), 1 <= E <= 1024, K and N multiples of 8 from 8 to 2^20, ONE matrix below 2 GiB (all of them together, and
- *      the rows, may be larger).  Errors, alignment and stream as above.  No workspace but ffuse_grouped_ffn's.
+ *      NULL), 1 <= E <= 1024, K and N multiples of 8 from 8 to 2^20, ONE matrix below 2 GiB: (K + 128) N elements (all of them
+ *      together, and the rows, may be larger).  Besides, work items are numbered by 32 bits: R < 2^31 - 512 and (R / 16 + E)
+ *      (max(K, N) / 32 + 1) < 2^31, and the gradient of the weights takes E ceil(K / 128) ceil(N / 128) < 2^23.  Anything else is
+ *      FFUSE_ERR_SHAPE.  Errors, alignment and stream as above.  No workspace but ffuse_grouped_ffn's.
  *
  *   ffuse_grouped_gemm      Y[r] = act(X[r] W[e]) (.* X[r] W3[e])      X[R][K], W[E][K][N], W3 like W or NULL, Y[R][N]
  *   ffuse_grouped_gemm_dx   dX[r] = dY[r] W[e]^T                        the plain product's gradients: of its input, dX[R][K],
@@ -259,12 +261,18 @@ int ffuse_grouped_ffn(int dtype, const void* X, const void* W1, const void* W3 /
  *      in between), scale[ceil(K/128)][ceil(M/block_rows)].  transpose = 1: the same of X^T: Q[K][Mp], scale[ceil(M/128)]
  *      [ceil(K/block_rows)].  The scale is the smallest power of two, 2^-126 at least, that brings the largest finite
  *      magnitude of the block to 448 or below (1 for a block of zeros): dividing by it is exact, the quotient is rounded once, to nearest
- *      even.  Infinities and NaN do not count for the scale and become NaN.  M >= 0, K a multiple of 8 up to 2^20.
+ *      even.  Infinities and NaN do not count for the scale and become NaN.  M from 0 to 2^31 - 1, K a multiple of 8 from 8 to 2^20,
+ *      (M / 64 + 1) (K / 128 + 1) < 2^23.
  *   ffuse_gemm_fp8       Y[m][n] = sum over blocks b of sa[b][m] sb[b][n / b_block] (sum over k in b of A[m][k] B[n][k])
  *      A[M][K], B[N][K] in e4m3, scales in fp32 (any, not only powers of two; sa sb is taken first) laid out as above, b_block 1
- *      or 128, Y[M][N] of type dtype (bf16 or fp16), rounded once.  M >= 0, K a multiple of 16, N of 8.  An inference product has A = rows of
- *      X by 1 x 128 and B = W^T by 128 x 128; its gradients dX = dY W^T (B = W untransposed) and dW = X^T dY (both
- *      operands transposed, by 1 x 128) are this product too.
+ *      or 128, Y[M][N] of type dtype (bf16 or fp16), rounded once.  M >= 0, K a multiple of 16 from 16 and N of 8 from 8, both up to
+ *      2^20, (K + 128) N < 2^31, M and the number of work items as above with E = 1.  (So a gradient of weights is over 2^20 tokens
+ *      at most, and over one at least.)
+ *      The sum over a block is taken by one matrix instruction: of each eight neighbouring k (8 i .. 8 i + 7) it aligns the products
+ *      with the largest of the eight and drops what lies more than 13 binary places below that one's leading bit, so that each of
+ *      the other seven is off by less than 2^-13 of the largest; the sums of the sixteen eights are added in fp32, and so are the blocks.
+ *      An inference product has A = rows of X by 1 x 128 and B = W^T by 128 x 128; its gradients dX = dY W^T (B = W
+ *      untransposed) and dW = X^T dY (both operands transposed, by 1 x 128) are this product too.
  *   ffuse_grouped_gemm_fp8   the same with the rows of A grouped by expert as above: B[E][N][K], sb[E][ceil(K/128)][...]. -- */
 int ffuse_fp8_quantize(int dtype, const void* X, int64_t M, int64_t K, int block_rows, int transpose, void* Q, float* scale,
                        void* stream);
