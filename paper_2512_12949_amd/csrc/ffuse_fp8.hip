@@ -28,7 +28,8 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
     asm volatile("s_mov_b32 m0, %1\n\tbuffer_load_dword %0, %2, 0 offen lds" :: "v"(voff), "s"(lds), "s"(r) : "memory", "m0");
 }
 
-// A stage is 128 k: BM + BN rows of 128 bytes, laid out as RowGemm's, and behind them their BM + BN scales of that block.
+// A stage is 128 k: BM + BN rows of 128 bytes, laid out as PairOperand lays out rows that are contiguous along the contraction, and
+// behind them their BM + BN scales of that block.
 // Computed transposed like the other block GEMMs: the MFMA "A" operand is B, so that a lane has four neighbouring
 // columns of one row of Y.
 //
@@ -41,6 +42,8 @@ __device__ __forceinline__ void lds_load4(__amdgpu_buffer_rsrc_t r, uint32_t vof
 //
 // What bounds it: 2.3 PFLOP/s at that size, the matrix pipes busy half of the time.  A copy of the kernel without loads in
 // the loop took 208 us instead of 240, one without fragment reads 242: the bytes from L2 to LDS, not LDS itself.
+// (256 x 256 takes all 256 registers; with scales of single columns four more, which are spilled outside the loop and reloaded
+// once an item.)
 template <typename T, int BM_, int BN_, int WM, int WN, int NS, int BLOCK_> struct Fp8Gemm {
     static constexpr int BM = BM_, BN = BN_, BLOCK = BLOCK_, NW = WM * WN, WMR = BM / WM, WNR = BN / WN, MT = WMR / 16, HT = WNR / 16;
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wave issues the same number of loads");
@@ -535,7 +538,7 @@ template <class G, class S> static hipError_t product(const Fp8Args& a, const Ti
     hipLaunchKernelGGL((fp8_product_kernel<G, S>), dim3(persistent_grid(items, cus, t.per_cu)), dim3(64 * G::NW), group_table_bytes(a.E), st, a, t.cost);
     return hipGetLastError();
 }
-// Tiles, and their times for a block of 128 k (4096 x 4096 x 16384)
+// Tiles, and their times for a block of 128 k, all set at one size (4096 x 4096 x 16384) with blocks of 128 of B's columns
 static constexpr Tile kFp8[] = {{256, 256, 1, 1.68f, 2.0f, 4, 0.36f}, {128, 256, 1, 1.00f, 2.0f, 4, 0.39f}, {128, 128, 1, 0.58f, 2.0f, 2, 0.64f},
                                 {64, 128, 1, 0.40f, 1.5f, 1, 1.0f},   {32, 128, 1, 0.33f, 1.5f, 1, 1.0f},   {64, 64, 2, 0.58f, 1.5f, 1, 1.0f}};
 template <typename T, int MT> static hipError_t stream(const Fp8Args& a, hipStream_t st) {

@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * WM * WN) void grouped_weights_kernel(GroupedAr
 // ---- launches ---------------------------------------------------------------------------------------------------
 // Tiles, and their times for 64 k, set on 16384 rows in eight uneven groups (4096 x 11008 gated, 11008 x 4096 plain, 4096 x 4096 for
 // the gradient of the input, whose operands need no transposing) and on 160 drawn problems of 1 to 16384 rows and 1 to 128
-// groups each, every tile timed on each: what is chosen takes 2 % more time than the best of them on average.  128 x 128, where
+// groups for each of the three tables, every tile timed on each: what is chosen takes 2 % more time than the best of them on average.  128 x 128, where
 // there are too few blocks of 128 x 256 for the CUs: 568 rows in five groups, 7168 x 3336, 75 us instead of 97 (plain) and 68
 // instead of 93 (input); 3184 in 23, 11656 x 576, 132 instead of 154 and 178 instead of 231.  A wave's part is 128 x 64 of the
 // largest (256 x 128 gated: 128 x 32 of either branch) and 32 x 32 of the small ones.
@@ -181,7 +181,9 @@ template <typename T, int BM, int BN, int WM, int WN, int NS> static hipError_t 
     hipLaunchKernelGGL((grouped_weights_kernel<T, BM, BN, WM, WN, NS>), dim3((unsigned)grid), dim3(64 * WM * WN), 0, st, a);
     return hipGetLastError();
 }
-// 256 x 256 takes 1.9 us for 64 rows, two of 128 x 128 side by side 1.2: four fill as many CUs twice as well, where there are few
+// 256 x 256 takes 1.9 us for 64 rows, two of 128 x 128 side by side 1.2: four fill as many CUs twice as well, where there are few.
+// (Times of long groups.  The 4 us beside them are the same for both, though the larger tile stores four times as much, and with few rows
+// a group the rule is off: 1501 rows in 12 groups, 1000 x 1352, 19 us where it expects 11.)
 template <typename T> static hipError_t weights_any(const GroupedArgs& a, int cus, hipStream_t st) {
     const auto items = [&](int b) { return (double)a.E * ((a.K + b - 1) / b) * ((a.N + b - 1) / b); };
     const double steps = (double)a.R / a.E / 64, big = items(256) / cus, small = items(128) / (2 * cus);
